@@ -281,7 +281,7 @@ def prepare(case, seed):
         heavy = torch.exp(1.5 * _normal(g, B, H_kv, slots))
         st.update(weights=heavy * (age / 512.0).clamp(max=1.0), new_table=st["spare"].view(B, per),
                   kept=torch.empty(B, H_kv, keep, dtype=torch.int32, device="cuda"), new_lens=torch.empty_like(st["lens"]),
-                  new_weights=torch.empty(B, H_kv, slots, device="cuda"))
+                  new_weights=torch.empty(B, H_kv, max(slots, per * PAGE), device="cuda"))
         return st
     w, s = case["window"], case["sinks"]
     n = case.get("N_q", 1)
@@ -467,7 +467,7 @@ def _plain_evict(st):
     src = kept.clamp(min=0)
     st["kept"].copy_(kept)
     st["new_lens"].copy_(n)
-    st["new_weights"].zero_()[..., :keep].copy_((st["weights"].gather(-1, src) * have)[..., :slots])
+    st["new_weights"].zero_()[..., :keep].copy_(st["weights"].gather(-1, src) * have)
     # the tokens, page by page: gathered from their slots, zeros past the end
     per = st["new_table"].shape[1]
     fill = (0, per * PAGE - keep)
@@ -675,7 +675,7 @@ def _exact_evict(st):
     w = st["weights"].cpu().double()
     B, H_kv, slots = w.shape
     kept = torch.full((B, H_kv, keep), -1, dtype=torch.int32)
-    out = torch.zeros(B, H_kv, slots, dtype=torch.float64)
+    out = torch.zeros(st["new_weights"].shape, dtype=torch.float64)
     lens = st["lens_host"]
     for b, L in enumerate(lens):
         for hk in range(H_kv):
