@@ -11,6 +11,8 @@
  *     with Delta_S (Eq. 11), the block-scaled FP4 MMA, online softmax (Eq. 3-6) with P
  *     quantized to E4M3 at the fixed scale 448, the FP8 PV MMA - for causal GQA
  *     prefill and for split-KV decode over a paged KV cache.
+ * For requests whose cache is bounded there are (not in the paper) the attention calls with a sliding window and sinks, and eviction
+ * of cached tokens by the attention weight that they have received.
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless its name starts with h_.  The caller owns
@@ -324,6 +326,67 @@ mpfa_status mpfa_decode(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, c
                         float v_scale, float softmax_scale, void *out_bf16, float *out_f32, void *workspace,
                         size_t workspace_bytes, int32_t *device_status, void *stream);
 
+/* ---- bounded caches: a sliding window with sinks, eviction by weight ------------------- */
+
+/* Attention with a sliding window and sinks (no counterpart in the paper).  The query at position p of its request sees key j when
+ *     j <= p  and  (j > p - window  or  j < sinks):
+ * the last `window` keys, its own among them, and the first `sinks` ones.  window >= 1, sinks >= 0, else MPFA_ERR_INVALID_ARG; a window
+ * of the whole context is causal attention.  Logits, softmax and P V are those of mpfa_prefill and mpfa_decode.  128-key blocks (counted
+ * from key 0) without a key that a query of the 128-row tile sees, in decode that the query sees, are left out of the traversal; the
+ * others are visited from the last to the first.  mpfa_set_prefill_arrangement does not concern these calls.
+ *
+ * mpfa_prefill_window: mpfa_prefill with this mask (causal, query i at position i + N_kv - N_q; rows without a visible key are zero).
+ * mpfa_prefill_paged_window: mpfa_prefill_paged with this mask.  mpfa_decode_window: mpfa_decode with this mask, the query at position
+ * seq_lens[b] - 1.
+ * Pages of which no key is visible to any query of a request are not read and their page-table entries not looked at, so they can be
+ * given away once the window has left them: with n queries a request needs the pages of keys < sinks and of keys > L - n - window.
+ * A hidden token's K and Delta_S may hold anything.  Its V may in decode; in the prefill calls a NaN in V reaches every row of each query
+ * tile that visits its block (mpfa_quantize_v writes one for a NaN in its input only).
+ * Here a seq_lens[b] above 64 * max_pages_per_req is treated as that bound in decode too.
+ * Partitions of mpfa_decode_window are 1024 keys of the blocks that are not left out, so its workspace follows the window:
+ * mpfa_decode_window_workspace_bytes().  max_pages_per_req of this section's calls is at most 2^24. */
+mpfa_status mpfa_prefill_window(const mpfa_fp4_tensor *h_q, const mpfa_fp4_tensor *h_k, const uint8_t *v_fp8,
+                                const void *delta_s_bf16, const mpfa_stats *h_stats, float v_scale, int window, int sinks,
+                                float softmax_scale, void *out_bf16, float *out_f32, int32_t *device_status, void *stream);
+mpfa_status mpfa_prefill_paged_window(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, const int32_t *page_table,
+                                      int max_pages_per_req, const int32_t *seq_lens, const int32_t *q_lens,
+                                      const mpfa_stats *h_stats, float v_scale, int window, int sinks, float softmax_scale,
+                                      void *out_bf16, float *out_f32, int32_t *device_status, void *stream);
+mpfa_status mpfa_decode_window(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, const int32_t *page_table,
+                               int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *h_stats, float v_scale,
+                               int window, int sinks, float softmax_scale, void *out_bf16, float *out_f32, void *workspace,
+                               size_t workspace_bytes, int32_t *device_status, void *stream);
+
+/* mpfa_decode that also keeps account of what each cached token receives (no counterpart in the paper):
+ *     weights[b, hk, j] += sum over the q heads h of kv head hk of 2^(lambda (S[h, j] - m[h])) / l[h]      for j < seq_lens[b],
+ * the softmax weights before P is rounded, in FP32.  weights is [B, H_kv, weights_stride] FP32 with weights_stride >= 64 *
+ * max_pages_per_req (else MPFA_ERR_INVALID_ARG); entries from seq_lens[b] on are left as they are.  A caller starts a token's sum at 0.
+ * The output is mpfa_decode's.  seq_lens[b] above 64 * max_pages_per_req is treated as that bound.  The workspace also holds the logits:
+ * mpfa_decode_weights_workspace_bytes(). */
+mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, const int32_t *page_table,
+                                int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *h_stats, float v_scale,
+                                float softmax_scale, float *weights, int weights_stride, void *out_bf16, float *out_f32,
+                                void *workspace, size_t workspace_bytes, int32_t *device_status, void *stream);
+
+/* Eviction from the paged cache by such sums (no counterpart in the paper).  Of a request with L = seq_lens[b] > keep tokens each kv head
+ * keeps its own `keep`: the first `sinks`, the last `recent`, and of the others the keep - sinks - recent with the largest weights[b, hk, :]
+ * (equal ones: the lowest slot first; NaN counts as less than every number).  A request of at most `keep` tokens keeps them all.  What is
+ * kept is copied in its order to the pages new_table[b, :] ([B, new_max_pages], new_max_pages >= ceil(keep / 64)) of the same pools; the
+ * rest of the last page is zeroed, pages after it are not touched.  The pages of page_table are only read, and can be given away
+ * afterwards; new_table must name none of them, and no page twice.
+ *   kept [B, H_kv, keep]  slot that each kept token had, ascending; -1 past the last.  For what the caller keeps per token, positions for
+ *                         instance, and scratch of the call.
+ *   new_lens [B]          min(L, keep).
+ *   new_weights [B, H_kv, new_weights_stride]  the kept tokens' weights, zeros after them (where new tokens' sums start).
+ * weights_stride >= 64 * max_pages_per_req, new_weights_stride >= keep, sinks + recent <= keep, and new_weights and new_lens overlap weights
+ * and seq_lens nowhere (else MPFA_ERR_INVALID_ARG).  seq_lens[b] above 64 * max_pages_per_req is treated as that bound, below 0 as 0.
+ * A page-table entry outside [0, num_pages) raises MPFA_DEV_BAD_PAGE: tokens of such a source page become zeros, a page of new_table is left
+ * out.  Decode works on the new pages as on any; since the kv heads keep different tokens, a slot no longer is a position. */
+mpfa_status mpfa_evict_paged(const mpfa_paged_kv *h_kv, const int32_t *page_table, int B, int max_pages_per_req,
+                             const int32_t *seq_lens, const float *weights, int weights_stride, int keep, int sinks, int recent,
+                             const int32_t *new_table, int new_max_pages, int32_t *kept, int32_t *new_lens, float *new_weights,
+                             int new_weights_stride, int32_t *device_status, void *stream);
+
 /* ---- measurement aid ------------------------------------------------------------------- */
 
 /* (Not a step of the paper's method: the roofline denominator for Sections 5.1-5.2's three MMA kinds.)
@@ -342,6 +405,8 @@ double mpfa_bench_mma_flops(int kind, int n_cols, int iters);
 size_t mpfa_quantize_workspace_bytes(int B, int H_q, int H_kv);
 size_t mpfa_quantize_workspace_min_bytes(int B, int H_q, int H_kv);
 size_t mpfa_decode_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req);
+size_t mpfa_decode_window_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req, int window, int sinks);
+size_t mpfa_decode_weights_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req);
 size_t mpfa_fp4_codes_bytes(int B, int H, int N);
 size_t mpfa_fp4_sf_bytes(int B, int H, int N);
 size_t mpfa_delta_s_bytes(int B, int H_q, int N_kv);

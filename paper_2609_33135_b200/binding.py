@@ -103,6 +103,10 @@ def load_library(path: str) -> ctypes.CDLL:
         L.mpfa_quantize_workspace_min_bytes.argtypes = [i, i, i]
         L.mpfa_decode_workspace_bytes.restype = sz
         L.mpfa_decode_workspace_bytes.argtypes = [i, i, i, i]
+        L.mpfa_decode_window_workspace_bytes.restype = sz
+        L.mpfa_decode_window_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        L.mpfa_decode_weights_workspace_bytes.restype = sz
+        L.mpfa_decode_weights_workspace_bytes.argtypes = [i, i, i, i]
         for name in ("mpfa_fp4_codes_bytes", "mpfa_fp4_sf_bytes", "mpfa_delta_s_bytes", "mpfa_v_fp8_bytes", "mpfa_v_fp4_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [i, i, i]
@@ -125,7 +129,12 @@ def load_library(path: str) -> ctypes.CDLL:
                            ("mpfa_prefill", [q4, q4, vp, vp, st, f, i, f, vp, vp, vp, vp]),
                            ("mpfa_prefill_variant", [q4, q4, vp, vp, st, f, i, f, i, vp, vp, vp, vp]),
                            ("mpfa_prefill_paged", [q4, pk, vp, i, vp, vp, st, f, f, vp, vp, vp, vp]),
-                           ("mpfa_decode", [q4, pk, vp, i, vp, st, f, f, vp, vp, vp, sz, vp, vp])):
+                           ("mpfa_decode", [q4, pk, vp, i, vp, st, f, f, vp, vp, vp, sz, vp, vp]),
+                           ("mpfa_prefill_window", [q4, q4, vp, vp, st, f, i, i, f, vp, vp, vp, vp]),
+                           ("mpfa_prefill_paged_window", [q4, pk, vp, i, vp, vp, st, f, i, i, f, vp, vp, vp, vp]),
+                           ("mpfa_decode_window", [q4, pk, vp, i, vp, st, f, i, i, f, vp, vp, vp, sz, vp, vp]),
+                           ("mpfa_decode_weights", [q4, pk, vp, i, vp, st, f, f, vp, i, vp, vp, vp, sz, vp, vp]),
+                           ("mpfa_evict_paged", [pk, vp, i, i, vp, vp, i, i, i, i, vp, i, vp, vp, vp, i, vp, vp])):
             typed, packed = getattr(L, name), L[name]   # two function objects of one symbol
             typed.restype = packed.restype = i
             typed.argtypes, packed.argtypes = args, [vp if t in (st, q4, pk) else t for t in args]
@@ -400,6 +409,77 @@ def mpfa_prefill_paged(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq_
                                   _ptr(seq_lens), _ptr(q_lens), sc, v_scale, softmax_scale, _ptr(out),
                                   _ptr(out_f32), _ptr(device_status), _stream())
     _check(rc, "mpfa_prefill_paged")
+
+
+def decode_window_workspace(B: int, H_q: int, H_kv: int, max_pages: int, window: int, sinks: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(256, lib().mpfa_decode_window_workspace_bytes(B, H_q, H_kv, max_pages, window, sinks)), dtype=torch.uint8,
+                       device=device)
+
+
+def decode_weights_workspace(B: int, H_q: int, H_kv: int, max_pages: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(256, lib().mpfa_decode_weights_workspace_bytes(B, H_q, H_kv, max_pages)), dtype=torch.uint8, device=device)
+
+
+def mpfa_prefill_window(q: Fp4Tensor, k: Fp4Tensor, v_fp8: torch.Tensor, delta: Optional[torch.Tensor], stats: Stats, v_scale: float,
+                        window: int, sinks: int, softmax_scale: float, out: torch.Tensor, out_f32: Optional[torch.Tensor],
+                        device_status: torch.Tensor) -> None:
+    """mpfa_prefill (causal) where each query sees the last `window` keys and the first `sinks`."""
+    rc = lib().packed_mpfa_prefill_window(q.packed_fp4(), k.packed_fp4(), _ptr(v_fp8), _ptr(delta), stats.packed_stats(), v_scale, window,
+                                          sinks, softmax_scale, _ptr(out), _ptr(out_f32), _ptr(device_status), _stream())
+    _check(rc, "mpfa_prefill_window")
+
+
+def mpfa_prefill_paged_window(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq_lens: torch.Tensor, stats: Stats, v_scale: float,
+                              window: int, sinks: int, softmax_scale: float, out: torch.Tensor, out_f32: Optional[torch.Tensor],
+                              device_status: torch.Tensor, q_lens: Optional[torch.Tensor] = None) -> None:
+    """mpfa_prefill_paged where each query sees the last `window` keys and the first `sinks`."""
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and seq_lens.dtype == torch.int32
+    assert q_lens is None or q_lens.dtype == torch.int32
+    rc = lib().packed_mpfa_prefill_paged_window(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),
+                                                _ptr(q_lens), stats.packed_stats(), v_scale, window, sinks, softmax_scale, _ptr(out),
+                                                _ptr(out_f32), _ptr(device_status), _stream())
+    _check(rc, "mpfa_prefill_paged_window")
+
+
+def mpfa_decode_window(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq_lens: torch.Tensor, stats: Stats, v_scale: float,
+                       window: int, sinks: int, softmax_scale: float, out: torch.Tensor, out_f32: Optional[torch.Tensor],
+                       workspace: torch.Tensor, device_status: torch.Tensor) -> None:
+    """mpfa_decode where the query sees the last `window` keys and the first `sinks`; workspace: decode_window_workspace()."""
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and seq_lens.dtype == torch.int32
+    rc = lib().packed_mpfa_decode_window(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),
+                                         stats.packed_stats(), v_scale, window, sinks, softmax_scale, _ptr(out), _ptr(out_f32),
+                                         _ptr(workspace), workspace.numel(), _ptr(device_status), _stream())
+    _check(rc, "mpfa_decode_window")
+
+
+def mpfa_decode_weights(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq_lens: torch.Tensor, stats: Stats, v_scale: float,
+                        softmax_scale: float, weights: torch.Tensor, out: torch.Tensor, out_f32: Optional[torch.Tensor],
+                        workspace: torch.Tensor, device_status: torch.Tensor) -> None:
+    """mpfa_decode that adds each key's softmax weights to weights [B, H_kv, >= 64 * pages] (float32); workspace:
+    decode_weights_workspace()."""
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and seq_lens.dtype == torch.int32
+    assert weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape[:2] == (q.B, kv.H_kv)
+    rc = lib().packed_mpfa_decode_weights(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),
+                                          stats.packed_stats(), v_scale, softmax_scale, _ptr(weights), weights.shape[2], _ptr(out),
+                                          _ptr(out_f32), _ptr(workspace), workspace.numel(), _ptr(device_status), _stream())
+    _check(rc, "mpfa_decode_weights")
+
+
+def mpfa_evict_paged(kv: PagedKV, page_table: torch.Tensor, seq_lens: torch.Tensor, weights: torch.Tensor, keep: int, sinks: int,
+                     recent: int, new_table: torch.Tensor, kept: torch.Tensor, new_lens: torch.Tensor, new_weights: torch.Tensor,
+                     device_status: torch.Tensor) -> None:
+    """Per request and kv head: the first `sinks` tokens, the last `recent` and the heaviest of the others, `keep` in all, copied to the
+    pages of new_table; kept [B, H_kv, keep] int32, new_lens [B] int32 and new_weights [B, H_kv, >= keep] float32 are written."""
+    for t in (page_table, seq_lens, new_table, kept, new_lens):
+        assert t.dtype == torch.int32 and t.is_contiguous()
+    for t in (weights, new_weights):
+        assert t.dtype == torch.float32 and t.is_contiguous() and t.shape[:2] == (page_table.shape[0], kv.H_kv)
+    B = page_table.shape[0]
+    assert new_table.shape[0] == seq_lens.numel() == new_lens.numel() == B and kept.shape == (B, kv.H_kv, keep)
+    rc = lib().packed_mpfa_evict_paged(kv.packed_paged(), _ptr(page_table), B, page_table.shape[1], _ptr(seq_lens), _ptr(weights),
+                                       weights.shape[2], keep, sinks, recent, _ptr(new_table), new_table.shape[1], _ptr(kept),
+                                       _ptr(new_lens), _ptr(new_weights), new_weights.shape[2], _ptr(device_status), _stream())
+    _check(rc, "mpfa_evict_paged")
 
 
 # ---------------------------------------------------------------------------------------

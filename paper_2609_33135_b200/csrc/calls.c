@@ -73,9 +73,24 @@ ENTRY(mpfa_prefill_paged, "pppipppffpppp", v[0].p, v[1].p, v[2].p, v[3].i, v[4].
 ENTRY(mpfa_decode, "pppippffpppzpp", v[0].p, v[1].p, v[2].p, v[3].i, v[4].p, v[5].p, v[6].f, v[7].f, v[8].p, v[9].p, v[10].p, v[11].z, v[12].p,
       v[13].p)
 
+/* The same for requests whose cache is bounded. */
+#define BOUNDED ENTRY
+BOUNDED(mpfa_prefill_window, "pppppfiifpppp", v[0].p, v[1].p, v[2].p, v[3].p, v[4].p, v[5].f, v[6].i, v[7].i, v[8].f, v[9].p, v[10].p,
+        v[11].p, v[12].p)
+BOUNDED(mpfa_prefill_paged_window, "pppipppfiifpppp", v[0].p, v[1].p, v[2].p, v[3].i, v[4].p, v[5].p, v[6].p, v[7].f, v[8].i, v[9].i, v[10].f,
+        v[11].p, v[12].p, v[13].p, v[14].p)
+BOUNDED(mpfa_decode_window, "pppippfiifpppzpp", v[0].p, v[1].p, v[2].p, v[3].i, v[4].p, v[5].p, v[6].f, v[7].i, v[8].i, v[9].f, v[10].p, v[11].p,
+        v[12].p, v[13].z, v[14].p, v[15].p)
+BOUNDED(mpfa_decode_weights, "pppippffpipppzpp", v[0].p, v[1].p, v[2].p, v[3].i, v[4].p, v[5].p, v[6].f, v[7].f, v[8].p, v[9].i, v[10].p, v[11].p,
+        v[12].p, v[13].z, v[14].p, v[15].p)
+BOUNDED(mpfa_evict_paged, "ppiippiiiipipppipp", v[0].p, v[1].p, v[2].i, v[3].i, v[4].p, v[5].p, v[6].i, v[7].i, v[8].i, v[9].i, v[10].p, v[11].i,
+        v[12].p, v[13].p, v[14].p, v[15].i, v[16].p, v[17].p)
+
 #define DEF(NAME) {#NAME, (PyCFunction)(void (*)(void))call_##NAME, METH_FASTCALL, NULL}
 static PyMethodDef entries[] = {DEF(mpfa_quantize_qk),     DEF(mpfa_quantize_qkv), DEF(mpfa_quantize_kv_paged), DEF(mpfa_append_kv_paged),
-                                DEF(mpfa_prefill), DEF(mpfa_prefill_paged), DEF(mpfa_decode)};
+                                DEF(mpfa_prefill), DEF(mpfa_prefill_paged), DEF(mpfa_decode),
+                                DEF(mpfa_prefill_window),  DEF(mpfa_prefill_paged_window), DEF(mpfa_decode_window), DEF(mpfa_decode_weights),
+                                DEF(mpfa_evict_paged)};
 
 static PyObject *bind(PyObject *module, PyObject *args) {
   const char *name;

@@ -51,6 +51,15 @@
 // 16 V producer, 1 QK issue (+ TMEM allocation), 2 PV issue, 3 rewrites the K scales of each block from
 // [token][8] into the 32 x 16-byte tiles tcgen05.cp expects, 4-7 and 8-11 the two softmax groups, 12-15 O (TMEM lane
 // quadrant = warp % 4).  Every wait is bounded.
+//
+// Three forms of it (template parameter MODE): every key (mpfa_decode); the keys of a sliding window and the first few
+// (mpfa_decode_window); every key, with the logits kept so that what each key received can be added to its running sum
+// (mpfa_decode_weights).
+//
+// Window.  Visible are the keys j >= low = L - window and j < sinks.  The blocks that hold one are numbered as if the blocks between the
+// two ranges did not exist (struct Span), and partitions, tickets and states count in those numbers; only addresses and masks use the
+// token's own index.  A page without a visible key is neither looked at nor copied, so its table entry may be stale, and of the V rows
+// of a page that is visible in part the others are zeros: a hidden token's V may be anything, NaN included, and 0 x NaN is not 0.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
@@ -59,6 +68,8 @@
 
 namespace mpfa {
 namespace {
+
+enum { ALL_KEYS = 0, WINDOW = 1, WEIGHTS = 2 };   // MODE
 
 constexpr int MAXG = 8;
 constexpr int NCOL = 16;          // MMA N: the GQA group padded to 16 columns
@@ -173,6 +184,13 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
+// The keys of a request as its work items count them.  Blocks [0, heads) are the sinks', then `shift` blocks are left out.
+struct Span {
+  int low;          // first key of the window
+  int heads, shift; // 0, 0 where nothing is left out
+  int len;          // keys, without those of the blocks that are left out
+};
+
 struct DecodeParams {
   const uint8_t *q_codes;  // tile layout, N = 1: row 0 of each (b, hq) tile
   const uint8_t *q_sf;
@@ -189,7 +207,32 @@ struct DecodeParams {
   int32_t *status;
   int B, H_q, H_kv, max_pages, num_pages, n_split;
   float softmax_scale, v_scale;
-  __device__ __forceinline__ int n_parts(int L) const { return min((max(L, 0) + DECODE_SPLIT - 1) / DECODE_SPLIT, n_split); }
+  int window, sinks;       // WINDOW
+  float *logits;           // WEIGHTS: [B, H_q, max_pages * 64]
+  float2 *final_ml;        // WEIGHTS: [B, H_q], (m, l) of the whole request
+  // A length beyond what the page table can address is cut to it in the forms that this file's later entry points use; mpfa_decode
+  // reports the pages that are missing.
+  template <int MODE>
+  __device__ __forceinline__ int length(int b) const {
+    const int L = seq_lens[b];
+    return MODE == ALL_KEYS ? L : min(L, max_pages * PAGE);
+  }
+  template <int MODE>
+  __device__ __forceinline__ Span span(int L) const {
+    if constexpr (MODE != WINDOW) return Span{0, 0, 0, L};
+    const int low = max(L - window, 0), heads = (min(sinks, low) + TILE - 1) / TILE, gap = low / TILE - heads;
+    return gap > 0 ? Span{low, heads, gap, L - gap * TILE} : Span{low, 0, 0, L};
+  }
+  template <int MODE>
+  __device__ __forceinline__ int n_parts(int L) const {
+    return min((max(span<MODE>(L).len, 0) + DECODE_SPLIT - 1) / DECODE_SPLIT, n_split);
+  }
+  // first token of a block
+  static __device__ __forceinline__ int block_key(const Span &sp, int block) { return (block + (block >= sp.heads ? sp.shift : 0)) * TILE; }
+  template <int MODE>
+  __device__ __forceinline__ bool visible(const Span &sp, int key, int L) const {
+    return key < L && (MODE != WINDOW || key >= sp.low || key < sinks);
+  }
 };
 
 // Work items (request, kv head, 1024-token partition) are handed out dynamically: one warp per CTA draws
@@ -243,9 +286,10 @@ struct DCtx {
 struct WorkIter {
   uint32_t n = 0;      // items taken so far
   int b, hk, sp, L, nblk;
+  Span span;
   // Whole warp, or the one thread that stands for its warp.  false: no more items (or the CTA is giving up).
-  template <bool ONE_THREAD = false>
-  __device__ bool next(const DCtx &cx, const int4 *ring) {
+  template <int MODE, bool ONE_THREAD = false>
+  __device__ bool next(const DecodeParams &p, const DCtx &cx, const int4 *ring) {
     const uint32_t slot = n % D_NITEM, parity = (n / D_NITEM) & 1;
     if (!(ONE_THREAD ? cx.wait(B_ITEM_FULL + slot, parity) : cx.wait_warp(B_ITEM_FULL + slot, parity))) return false;
     const int4 it = ring[slot];
@@ -256,7 +300,8 @@ struct WorkIter {
       cx.warp_arrive(B_ITEM_EMPTY + slot);
     ++n;
     b = it.x, hk = it.y, sp = it.z, L = it.w;
-    nblk = (min(L - sp * DECODE_SPLIT, DECODE_SPLIT) + TILE - 1) / TILE;
+    span = p.span<MODE>(L);
+    nblk = (min(span.len - sp * DECODE_SPLIT, DECODE_SPLIT) + TILE - 1) / TILE;
     return true;
   }
 };
@@ -266,11 +311,21 @@ struct WorkIter {
 __device__ __forceinline__ void lookup_pages(const DecodeParams &p, const WorkIter &w, int lane, int &pid0, int &pid1) {
   pid0 = -1, pid1 = -1;
   if (lane < w.nblk) {
-    const int pg = (w.sp * DECODE_SPLIT + lane * TILE) / PAGE;
+    const int pg = DecodeParams::block_key(w.span, w.sp * MAXBLK + lane) / PAGE;
     const int32_t *row = p.page_table + (size_t)w.b * p.max_pages;
     if (pg < p.max_pages) pid0 = row[pg];
     if (pg + 1 < p.max_pages) pid1 = row[pg + 1];
   }
+}
+
+// The V rows [0, hide) and [show, 64) of a page; one copy where nothing lies between.
+__device__ __forceinline__ void load_rows(uint32_t dst, const uint8_t *src, int hide, int show, uint32_t bar) {
+  if (hide == show) {
+    bulk_load(dst, src, PAGE * HEAD_DIM, bar);
+    return;
+  }
+  if (hide > 0) bulk_load(dst, src, (uint32_t)hide * HEAD_DIM, bar);
+  if (show < PAGE) bulk_load(dst + (uint32_t)show * HEAD_DIM, src + show * HEAD_DIM, (uint32_t)(PAGE - show) * HEAD_DIM, bar);
 }
 
 // Registers of a thread: a block of 256 threads and 64 registers of the small kernels before and after fits on an SM beside a CTA of this
@@ -278,7 +333,7 @@ __device__ __forceinline__ void lookup_pages(const DecodeParams &p, const WorkIt
 // R <= 72.  Groups of up to four heads need no more (a bound of 896 threads asks for it); the function call in the waits had raised
 // them to 80 and more.  Append, query and decode at 80 / 72: 16 requests of 16..128 tokens, 16:16 heads 17.9 / 14.8 us; 100 of 100..700, 8:2
 // 23.4 / 19.0; 64 of 100..1000, 32:8 31.6 / 30.0.  Larger groups spill there (groups of eight, 64 of 100..2000 21.0 / 21.9).
-template <int G>
+template <int G, int MODE>
 __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kernel(const __grid_constant__ DecodeParams p) {
   extern __shared__ uint8_t dsm_raw[];
   uint8_t *dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~uintptr_t(1023));
@@ -343,7 +398,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
   int32_t *len_tab = reinterpret_cast<int32_t *>(dsm + D_OFF_LEN);
   float *lam_tab = reinterpret_cast<float *>(dsm + D_OFF_LAM);
   for (int i = threadIdx.x; i < min(p.B, D_MAXREQ); i += D_THREADS) {
-    len_tab[i] = p.seq_lens[i];
+    len_tab[i] = p.length<MODE>(i);
     lam_tab[i] = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[i]), p.k_gscale[i]);
   }
   fence_proxy_async_smem();
@@ -367,7 +422,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       // pre[b] = items of requests 0..b-1: every lane sums a contiguous run of requests, the warp scans the runs
       const int per = (p.B + 31) / 32, lo = min(p.B, lane * per), hi = min(p.B, lo + per);
       int run = 0;
-      for (int i = lo; i < hi; ++i) run += p.n_parts(len_tab[i]) * p.H_kv;
+      for (int i = lo; i < hi; ++i) run += p.n_parts<MODE>(len_tab[i]) * p.H_kv;
       int incl = run;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -377,7 +432,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       int acc = incl - run;
       for (int i = lo; i < hi; ++i) {
         pre[i] = acc;
-        acc += p.n_parts(len_tab[i]) * p.H_kv;
+        acc += p.n_parts<MODE>(len_tab[i]) * p.H_kv;
       }
       total = (uint32_t)__shfl_sync(0xffffffffu, incl, 31);
       if (lane == 31) pre[p.B] = (int)total;
@@ -406,14 +461,14 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
               const int mid = (lo + hi) >> 1;
               if ((uint32_t)pre[mid] <= tkt) lo = mid; else hi = mid;
             }
-            const int L = len_tab[lo], nsp = p.n_parts(L);
+            const int L = len_tab[lo], nsp = p.n_parts<MODE>(L);
             const int r = (int)tkt - pre[lo];
             item = make_int4(lo, r / nsp, r % nsp, L);
             break;
           }
           const int sp = (int)(tkt % (uint32_t)p.n_split), r = (int)(tkt / (uint32_t)p.n_split);
-          const int b = r / p.H_kv, L = p.seq_lens[b];
-          if (L - sp * DECODE_SPLIT > 0) {
+          const int b = r / p.H_kv, L = p.length<MODE>(b);
+          if (p.span<MODE>(L).len - sp * DECODE_SPLIT > 0) {
             item = make_int4(b, r % p.H_kv, sp, L);
             break;
           }
@@ -426,7 +481,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       item.y = __shfl_sync(0xffffffffu, item.y, 0);
       item.z = __shfl_sync(0xffffffffu, item.z, 0);
       item.w = __shfl_sync(0xffffffffu, item.w, 0);
-      prev_short = item.w - item.z * DECODE_SPLIT <= DECODE_SPLIT / 2;
+      prev_short = p.span<MODE>(item.w).len - item.z * DECODE_SPLIT <= DECODE_SPLIT / 2;
       const size_t head0 = (size_t)item.x * p.H_q + (size_t)item.y * G;
       uint4 qv = make_uint4(0u, 0u, 0u, 0u);
       uint32_t qs0 = 0, qs1 = 0;
@@ -469,23 +524,38 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     const int b_full = is_k ? B_K_FULL : B_V_FULL, b_empty = is_k ? B_K_EMPTY : B_V_EMPTY;
     static_assert(D_NK % 2 == 0, "each K producer has its own stages");
     int pc0 = -1, pc1 = -1, pn0 = -1, pn1 = -1;
-    bool vw = w.next(cx, ring), vn = false;
+    bool vw = w.next<MODE>(p, cx, ring), vn = false;
     if (vw) lookup_pages(p, w, lane, pc0, pc1);
     for (; ok && vw; ++j) {
       if (warp == 0) cx.warp_arrive(B_DRAW + (j & 1));
       // Nothing can be done with V before the first item's softmax, and while all CTAs start at once its copies only keep K waiting, of
       // which warp 17's last block may still be to come.
       if (!is_k && j == 0) ok = cx.wait_warp(B_V_GO, 0);
-      const bool in = lane < w.nblk, want1 = w.sp * DECODE_SPLIT + lane * TILE + PAGE < w.L;
-      const bool has0 = in && pc0 >= 0 && pc0 < p.num_pages, has1 = in && want1 && pc1 >= 0 && pc1 < p.num_pages;
-      if (in && (!has0 || (want1 && !has1))) atomicOr(p.status, MPFA_DEV_BAD_PAGE);
+      const int key0 = DecodeParams::block_key(w.span, w.sp * MAXBLK + lane);
+      const bool in = lane < w.nblk;
+      bool want0 = true, want1 = key0 + PAGE < w.L;
+      // rows of the two pages between the sinks' end and the window's beginning: of a page that is all of it nothing is wanted, of another
+      // one V takes these as zeros
+      int hide0 = 0, show0 = 0, hide1 = 0, show1 = 0;
+      if constexpr (MODE == WINDOW) {
+        hide0 = min(max(p.sinks - key0, 0), PAGE), show0 = min(max(w.span.low - key0, hide0), PAGE);
+        hide1 = min(max(p.sinks - key0 - PAGE, 0), PAGE), show1 = min(max(w.span.low - key0 - PAGE, hide1), PAGE);
+        want0 = show0 - hide0 < PAGE, want1 = want1 && show1 - hide1 < PAGE;
+      }
+      const bool has0 = in && want0 && pc0 >= 0 && pc0 < p.num_pages, has1 = in && want1 && pc1 >= 0 && pc1 < p.num_pages;
+      if (in && ((want0 && !has0) || (want1 && !has1))) atomicOr(p.status, MPFA_DEV_BAD_PAGE);
+      if constexpr (MODE == WINDOW) {
+        if (!has0) hide0 = 0, show0 = PAGE;
+        if (!has1) hide1 = 0, show1 = PAGE;
+      }
       const size_t slab0 = (size_t)(has0 ? pc0 : 0) * p.H_kv + w.hk, slab1 = (size_t)(has1 ? pc1 : 0) * p.H_kv + w.hk;
       const uint8_t *const big0 = is_k ? p.k_codes + slab0 * 4096 : p.v_fp8 + slab0 * 8192;
       const uint8_t *const big1 = is_k ? p.k_codes + slab1 * 4096 : p.v_fp8 + slab1 * 8192;
       const uint8_t *const sf0 = p.k_sf + slab0 * 512, *const sf1 = p.k_sf + slab1 * 512;
       const __nv_bfloat16 *const del0 = p.delta + slab0 * (G * PAGE), *const del1 = p.delta + slab1 * (G * PAGE);
-      const uint32_t bytes = ((has0 ? 1u : 0u) + (has1 ? 1u : 0u)) * page_bytes;
-      const uint32_t absent = __ballot_sync(0xffffffffu, in && !(has0 && has1));
+      uint32_t bytes = ((has0 ? 1u : 0u) + (has1 ? 1u : 0u)) * page_bytes;
+      if (MODE == WINDOW && !is_k) bytes = (uint32_t)(2 * PAGE - (show0 - hide0) - (show1 - hide1)) * HEAD_DIM;
+      const uint32_t absent = __ballot_sync(0xffffffffu, in && (MODE == WINDOW ? show0 > hide0 || show1 > hide1 : !(has0 && has1)));
       for (int t = 0; ok && t < w.nblk; ++t, ++c) {
         const uint32_t st = c % n_ring;
         const bool mine = !is_k || (c & 1) == (warp == 17 ? 1u : 0u);
@@ -497,13 +567,21 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         const uint32_t full = cx.bar(b_full + st);
         if (!is_k && (absent >> u & 1u)) {
           // a page that is not there contributes P_hat = 0 times V: V must be finite, so zero it
-          const bool h0 = __shfl_sync(0xffffffffu, has0, u), h1 = __shfl_sync(0xffffffffu, has1, u);
           uint8_t *stage = dsm + D_OFF_V + st * VST_BYTES;
+          if constexpr (MODE == WINDOW) {   // a token's V is one row of 128 bytes
+            const int a0 = __shfl_sync(0xffffffffu, hide0, u), b0 = __shfl_sync(0xffffffffu, show0, u);
+            const int a1 = __shfl_sync(0xffffffffu, hide1, u), b1 = __shfl_sync(0xffffffffu, show1, u);
+            for (int o = a0 * HEAD_DIM + lane * 16; o < b0 * HEAD_DIM; o += 512) *reinterpret_cast<uint4 *>(stage + o) = make_uint4(0u, 0u, 0u, 0u);
+            for (int o = a1 * HEAD_DIM + lane * 16; o < b1 * HEAD_DIM; o += 512)
+              *reinterpret_cast<uint4 *>(stage + 8192 + o) = make_uint4(0u, 0u, 0u, 0u);
+          } else {
+            const bool h0 = __shfl_sync(0xffffffffu, has0, u), h1 = __shfl_sync(0xffffffffu, has1, u);
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            if (half == 0 ? h0 : h1) continue;
-            for (int i = 0; i < 16; ++i)
-              *reinterpret_cast<uint4 *>(stage + half * 8192 + i * 512 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+            for (int half = 0; half < 2; ++half) {
+              if (half == 0 ? h0 : h1) continue;
+              for (int i = 0; i < 16; ++i)
+                *reinterpret_cast<uint4 *>(stage + half * 8192 + i * 512 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -529,14 +607,19 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
             }
           } else {
             const uint32_t dst = sbase + D_OFF_V + st * VST_BYTES;
-            if (has0) bulk_load(dst, big0, 8192, full);
-            if (has1) bulk_load(dst + 8192, big1, 8192, full);
+            if constexpr (MODE == WINDOW) {
+              load_rows(dst, big0, hide0, show0, full);
+              load_rows(dst + 8192, big1, hide1, show1, full);
+            } else {
+              if (has0) bulk_load(dst, big0, 8192, full);
+              if (has1) bulk_load(dst + 8192, big1, 8192, full);
+            }
           }
         }
         __syncwarp();
         if (t == max(0, w.nblk - 3)) {
           wn = w;
-          vn = wn.next(cx, ring);
+          vn = wn.next<MODE>(p, cx, ring);
           if (vn) lookup_pages(p, wn, lane, pn0, pn1);
         }
       }
@@ -566,7 +649,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       WorkIter w;
       uint32_t kc = 0, j = 0;
       bool ok = true;
-      while (ok && w.next<true>(cx, ring)) {
+      while (ok && w.next<MODE, true>(p, cx, ring)) {
         const uint32_t par = j & 1;
         ok = cx.wait(B_Q_READY + par, (j >> 1) & 1);
         if (ok && j >= 2) ok = cx.wait(B_S_FREE + par, ((j >> 1) - 1) & 1);   // scores of item j-2 have been read
@@ -617,7 +700,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       WorkIter w;
       uint32_t vc = 0, j = 0;
       bool ok = true;
-      while (ok && w.next<true>(cx, ring)) {
+      while (ok && w.next<MODE, true>(p, cx, ring)) {
         const uint32_t par = j & 1;
         ok = cx.wait(B_P_READY + par, (j >> 1) & 1);
         if (ok && j >= 1) ok = cx.wait(B_O_FREE, (j - 1) & 1);   // the previous item's O has been read
@@ -648,7 +731,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     WorkIter w;
     uint32_t kc = 0;
     bool ok = true;
-    while (ok && w.next(cx, ring)) {
+    while (ok && w.next<MODE>(p, cx, ring)) {
       for (int t = 0; t < w.nblk; ++t, ++kc) {
         const uint32_t st = kc % D_NK;
         ok = cx.wait_warp(B_K_FULL + st, (kc / D_NK) & 1);
@@ -675,14 +758,13 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     constexpr int GP = G <= 4 ? 4 : 8, TPV = 32 / GP, NV = MAXBLK / TPV;   // heads padded; blocks to a warp's lanes; such sets
     bool ok = true;
     WorkIter w;
-    for (uint32_t j = 0; ok && w.next(cx, ring); ++j) {
+    for (uint32_t j = 0; ok && w.next<MODE>(p, cx, ring); ++j) {
       const uint32_t par = j & 1, ph = (j >> 1) & 1;
       const uint32_t tS = tm + TM_S + par * (MAXBLK * 16) + tlane;
       uint8_t *const pt = dsm + D_OFF_P + par * MAXBLK * 1024 + (r & 15);
       float *xm = xmax + par * MAXBLK * MAXG * 4, *wt = wtab + par * MAXBLK * MAXG, *xlg = xl + par * 8 * MAXG;
       const float lam = w.b < D_MAXREQ ? lam_tab[w.b]
                                        : __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[w.b]), p.k_gscale[w.b]);
-      const int k_part = w.sp * DECODE_SPLIT;
       // ---- all scores of the item at once.  They are read from tensor memory twice, once for the maxima and once for the
       // exponentials: held in registers in between, MAXBLK x G of them and as many maxima went to local memory for groups
       // of five heads and more (24 us per item instead of 6).
@@ -701,7 +783,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         for (int u = 0; u < CH; ++u) {
           const int t = t0 + 2 * u;
           if (t < w.nblk) {
-            const bool valid = k_part + (w.nblk - 1 - t) * TILE + r < w.L;
+            const bool valid = p.visible<MODE>(w.span, DecodeParams::block_key(w.span, w.sp * MAXBLK + w.nblk - 1 - t) + r, w.L);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               const float wm = warp_max(valid ? __uint_as_float(sr[u][g]) : -INFINITY);
@@ -755,8 +837,16 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
           for (int u = 0; u < CH; ++u) {
             const int t = v * TPV + t0 + 2 * u;
             if (t < w.nblk) {
-              const bool valid = k_part + (w.nblk - 1 - t) * TILE + r < w.L;
+              const bool valid = p.visible<MODE>(w.span, DecodeParams::block_key(w.span, w.sp * MAXBLK + w.nblk - 1 - t) + r, w.L);
               float pq[G + 1];
+              if constexpr (MODE == WEIGHTS) {
+                if (valid) {
+                  const size_t slots = (size_t)p.max_pages * PAGE;
+                  float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + (w.sp * MAXBLK + w.nblk - 1 - t) * TILE + r;
+#pragma unroll
+                  for (int g = 0; g < G; ++g) x[g * slots] = __uint_as_float(sr[u][g]);
+                }
+              }
 #pragma unroll
               for (int g = 0; g < G; ++g) {
                 const float c = __shfl_sync(0xffffffffu, nml[v], (t0 + 2 * u) * GP + g), wg = __shfl_sync(0xffffffffu, wl[v], (t0 + 2 * u) * GP + g);
@@ -796,7 +886,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     const uint32_t tO = tm + TM_O + ((uint32_t)(quad * 32) << 16);
     bool ok = true;
     WorkIter w;
-    for (uint32_t j = 0; ok && w.next(cx, ring); ++j) {
+    for (uint32_t j = 0; ok && w.next<MODE>(p, cx, ring); ++j) {
       const int par = j & 1;
       const float *wt = wtab + par * MAXBLK * MAXG, *xlg = xl + par * 8 * MAXG;
       ok = cx.wait_warp(B_P_READY + par, (j >> 1) & 1) && cx.wait_warp(B_O_FULL, j & 1);   // the item's tables; its accumulators
@@ -828,10 +918,11 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       cx.warp_arrive(B_O_FREE);
       cx.warp_arrive(B_T_FREE + par);
       const size_t head0 = (size_t)w.b * p.H_q + (size_t)w.hk * G;
-      const int n_parts = p.n_parts(w.L);
+      const int n_parts = p.n_parts<MODE>(w.L);
       if (n_parts == 1) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
+          if (MODE == WEIGHTS && r == g) p.final_ml[head0 + g] = make_float2(m[g], l[g]);
           const float y = l[g] > 0.0f ? __fmul_rn(__fdiv_rn(acc[g], __fmul_rn(448.0f, l[g])), p.v_scale) : 0.0f;
           p.out[(head0 + g) * HEAD_DIM + r] = __float2bfloat16_rn(y);
           if (p.out_f32) p.out_f32[(head0 + g) * HEAD_DIM + r] = y;
@@ -864,6 +955,7 @@ __global__ void decode_prep_kernel(unsigned int *ticket) {
 // w + 4, ... in ascending order, a lane four channels (one 512-byte row per warp and load, four rows in flight), and the
 // four sums are added in warp order: a fixed order, so the result is reproducible.  128 threads of at most 56 registers
 // fit beside a CTA of the split kernel.  Requests of one partition or without keys are complete already.
+template <int MODE>
 __global__ void __launch_bounds__(128, 9) decode_merge_kernel(const __grid_constant__ DecodeParams p) {
   __shared__ float s_l[4];
   __shared__ __align__(16) float s_o[4][HEAD_DIM];
@@ -889,7 +981,7 @@ __global__ void __launch_bounds__(128, 9) decode_merge_kernel(const __grid_const
       x[u] = po[(size_t)s * (HEAD_DIM / 4)];
     }
   const float first_max = ml[min(lane, p.n_split - 1)].x;
-  const int n = p.n_parts(p.seq_lens[b]);
+  const int n = p.n_parts<MODE>(p.length<MODE>(b));
   const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
   if (n <= 1) return;
   float M = lane < n ? first_max : -INFINITY;
@@ -925,6 +1017,7 @@ __global__ void __launch_bounds__(128, 9) decode_merge_kernel(const __grid_const
   const int c = threadIdx.x;
   const float lt = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]), ot = (s_o[0][c] + s_o[1][c]) + (s_o[2][c] + s_o[3][c]);
   const float y = lt > 0.0f ? __fmul_rn(__fdiv_rn(ot, __fmul_rn(448.0f, lt)), p.v_scale) : 0.0f;
+  if (MODE == WEIGHTS && c == 0) p.final_ml[head] = make_float2(M, lt);
   p.out[head * HEAD_DIM + c] = __float2bfloat16_rn(y);
   if (p.out_f32) p.out_f32[head * HEAD_DIM + c] = y;
 }
@@ -933,6 +1026,7 @@ __global__ void __launch_bounds__(128, 9) decode_merge_kernel(const __grid_const
 // exchange.  (Four warps of which each had one state, append + query + decode: 256 requests of 100..2000 tokens 126 us, now 122.5; 64
 // of 100..4000 66 both ways.)
 constexpr int FEW_PARTS = 4;
+template <int MODE>
 __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_constant__ DecodeParams p) {
   grid_dependency_wait();
   const int head = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -948,7 +1042,7 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
     a[s] = ml[at];
     x[s] = po[(size_t)at * (HEAD_DIM / 4)];
   }
-  const int n = p.n_parts(p.seq_lens[b]);
+  const int n = p.n_parts<MODE>(p.length<MODE>(b));
   const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
   if (n <= 1) return;
   float M = -INFINITY;
@@ -966,6 +1060,7 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
     o[2] = __fmaf_rn(w, x[s].z, o[2]);
     o[3] = __fmaf_rn(w, x[s].w, o[3]);
   }
+  if (MODE == WEIGHTS && lane == 0) p.final_ml[head] = make_float2(M, l);
   __align__(8) __nv_bfloat16 h[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -985,34 +1080,81 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
   }
 }
 
+// What each key received: weights[b, kv head, j] += sum over the group's heads of 2^(lam (S_j - m)) / l, in FP32 from the logits that the
+// split kernel kept and the (m, l) of the whole request.  A thread takes four keys, a block chunks of 1024, heads in ascending order: one
+// writer per sum, a fixed order.  Bound by memory: 4 G bytes of logits per key read back (mostly from L2), 8 of the sum.
+constexpr int W_KEYS = 1024;
+__global__ void __launch_bounds__(W_KEYS / 4) decode_weights_kernel(const __grid_constant__ DecodeParams p, float *weights, size_t stride) {
+  grid_dependency_wait();
+  const int hk = blockIdx.y, b = blockIdx.z, G = p.H_q / p.H_kv;
+  const int L = p.length<WEIGHTS>(b);
+  const size_t slots = (size_t)p.max_pages * PAGE, head0 = (size_t)b * p.H_q + (size_t)hk * G;
+  const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
+  float *const sum = weights + ((size_t)b * p.H_kv + hk) * stride;
+  for (int j = (int)blockIdx.x * W_KEYS + (int)threadIdx.x * 4; j < L; j += (int)gridDim.x * W_KEYS) {
+    float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g = 0; g < G; ++g) {
+      const float2 ml = p.final_ml[head0 + g];
+      const float4 x = *reinterpret_cast<const float4 *>(p.logits + (head0 + g) * slots + j);
+      const float c = -__fmul_rn(ml.x, lam), inv = ml.y > 0.0f ? __frcp_rn(ml.y) : 0.0f;
+      w[0] = __fmaf_rn(ex2_approx(__fmaf_rn(x.x, lam, c)), inv, w[0]);
+      w[1] = __fmaf_rn(ex2_approx(__fmaf_rn(x.y, lam, c)), inv, w[1]);
+      w[2] = __fmaf_rn(ex2_approx(__fmaf_rn(x.z, lam, c)), inv, w[2]);
+      w[3] = __fmaf_rn(ex2_approx(__fmaf_rn(x.w, lam, c)), inv, w[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (j + i < L) sum[j + i] = __fadd_rn(sum[j + i], w[i]);
+  }
+}
+
 }  // namespace
 }  // namespace mpfa
 
 using namespace mpfa;
 
-// Workspace: partition accumulators, partition (m, l), work counter; each part 256-byte aligned.
+// Workspace: partition accumulators, partition (m, l), work counter; with weights the request's (m, l) and the logits; each part 256-byte
+// aligned.
 struct DecodeWorkspace {
-  size_t ml, ticket, bytes;
+  size_t ml, ticket, final_ml, logits, bytes;
 };
-static DecodeWorkspace decode_workspace(int B, int H_q, size_t n_split) {
+static DecodeWorkspace decode_workspace(int B, int H_q, size_t n_split, size_t slots = 0) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   DecodeWorkspace w;
   w.ml = up((size_t)B * H_q * n_split * HEAD_DIM * sizeof(float));
   w.ticket = w.ml + up((size_t)B * H_q * n_split * sizeof(float2));
-  w.bytes = w.ticket + 256;
+  w.final_ml = w.ticket + 256;
+  w.logits = w.final_ml + (slots ? up((size_t)B * H_q * sizeof(float2)) : 0);
+  w.bytes = w.logits + (size_t)B * H_q * slots * sizeof(float);
   return w;
+}
+static size_t all_splits(int max_pages) { return ((size_t)max_pages * PAGE + DECODE_SPLIT - 1) / DECODE_SPLIT; }
+// Partitions of the blocks that a window and the sinks can reach: `window` keys in a row touch (window + 126) / 128 + 1 blocks at most.
+static size_t window_splits(int max_pages, int window, int sinks) {
+  const size_t all = ((size_t)max_pages * PAGE + TILE - 1) / TILE;
+  const size_t some = ((size_t)sinks + TILE - 1) / TILE + ((size_t)window + TILE - 2) / TILE + 1;
+  return ((some < all ? some : all) + MAXBLK - 1) / MAXBLK;
 }
 
 extern "C" size_t mpfa_decode_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req) {
   if (B <= 0 || H_q <= 0 || H_kv <= 0 || max_pages_per_req <= 0) return 0;
-  const size_t n_split = ((size_t)max_pages_per_req * PAGE + DECODE_SPLIT - 1) / DECODE_SPLIT;
-  return decode_workspace(B, H_q, n_split).bytes;
+  return decode_workspace(B, H_q, all_splits(max_pages_per_req)).bytes;
 }
 
-extern "C" mpfa_status mpfa_decode(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
-                                   int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *st, float v_scale,
-                                   float softmax_scale, void *out_bf16, float *out_f32, void *workspace,
-                                   size_t workspace_bytes, int32_t *device_status, void *stream) {
+extern "C" size_t mpfa_decode_window_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req, int window, int sinks) {
+  if (B <= 0 || H_q <= 0 || H_kv <= 0 || max_pages_per_req <= 0 || window <= 0 || sinks < 0) return 0;
+  return decode_workspace(B, H_q, window_splits(max_pages_per_req, window, sinks)).bytes;
+}
+
+extern "C" size_t mpfa_decode_weights_workspace_bytes(int B, int H_q, int H_kv, int max_pages_per_req) {
+  if (B <= 0 || H_q <= 0 || H_kv <= 0 || max_pages_per_req <= 0) return 0;
+  return decode_workspace(B, H_q, all_splits(max_pages_per_req), (size_t)max_pages_per_req * PAGE).bytes;
+}
+
+// The arguments that the three calls share: checked, and put into the launch parameters.
+static mpfa_status decode_params(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table, int max_pages_per_req,
+                                 const int32_t *seq_lens, const mpfa_stats *st, float v_scale, float softmax_scale, void *out_bf16,
+                                 float *out_f32, void *workspace, int32_t *device_status, DecodeParams *params) {
   if (!q || !kv || !page_table || !seq_lens || !st || !out_bf16 || !workspace || !device_status)
     return MPFA_ERR_INVALID_ARG;
   if (!q->codes || !q->sf || q->B <= 0 || q->H <= 0 || q->N != 1 || max_pages_per_req <= 0)
@@ -1021,20 +1163,10 @@ extern "C" mpfa_status mpfa_decode(const mpfa_fp4_tensor *q, const mpfa_paged_kv
     return MPFA_ERR_INVALID_ARG;
   if (!(softmax_scale > 0.0f) || !(v_scale > 0.0f)) return MPFA_ERR_INVALID_ARG;
   if (kv->page_size != PAGE) return MPFA_ERR_UNSUPPORTED;
-  const int B = q->B, H_q = q->H, H_kv = kv->H_kv;
+  const int H_q = q->H, H_kv = kv->H_kv;
   if (H_kv <= 0 || kv->H_q != H_q) return MPFA_ERR_INVALID_ARG;
   if (H_q % H_kv != 0 || H_q / H_kv > MAXG) return MPFA_ERR_UNSUPPORTED;
-  const size_t n_split = ((size_t)max_pages_per_req * PAGE + DECODE_SPLIT - 1) / DECODE_SPLIT;
-  const DecodeWorkspace ws = decode_workspace(B, H_q, n_split);
-  if (workspace_bytes < ws.bytes) return MPFA_ERR_WORKSPACE;
-  if ((size_t)B * H_kv * n_split > 0x7FFFFFFFull || B > 65535) return MPFA_ERR_UNSUPPORTED;
-  if (!aligned(q->codes, 16) || !aligned(q->sf, 16) || !aligned(kv->k_codes, 256) || !aligned(kv->k_sf, 256) ||
-      !aligned(kv->v_fp8, 256) || !aligned(kv->delta_s_bf16, 256) || !aligned(workspace, 16))
-    return MPFA_ERR_ALIGNMENT;
-  int dev = 0, n_sm = 0;
-  mpfa_status rc = device_info(&dev, &n_sm);
-  if (rc != MPFA_OK) return rc;
-  DecodeParams p;
+  DecodeParams &p = *params;
   p.q_codes = q->codes;
   p.q_sf = q->sf;
   p.k_codes = kv->k_codes;
@@ -1046,42 +1178,127 @@ extern "C" mpfa_status mpfa_decode(const mpfa_fp4_tensor *q, const mpfa_paged_kv
   p.q_gscale = st->q_gscale;
   p.k_gscale = st->k_gscale;
   p.part_o = static_cast<float *>(workspace);
-  p.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + ws.ml);
   p.out = static_cast<__nv_bfloat16 *>(out_bf16);
   p.out_f32 = out_f32;
   p.status = device_status;
-  p.B = B;
+  p.B = q->B;
   p.H_q = H_q;
   p.H_kv = H_kv;
   p.max_pages = max_pages_per_req;
   p.num_pages = kv->num_pages;
-  p.n_split = (int)n_split;
   p.softmax_scale = softmax_scale;
   p.v_scale = v_scale;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const size_t items = (size_t)B * H_kv * n_split;
+  p.window = 0;
+  p.sinks = 0;
+  p.logits = nullptr;
+  p.final_ml = nullptr;
+  return MPFA_OK;
+}
+
+// Where the workspace's parts are, and what is found on the host only now: sizes, alignment, the device.
+static mpfa_status decode_place(DecodeParams &p, size_t n_split, size_t slots, size_t workspace_bytes, int *n_sm) {
+  const DecodeWorkspace ws = decode_workspace(p.B, p.H_q, n_split, slots);
+  if (workspace_bytes < ws.bytes) return MPFA_ERR_WORKSPACE;
+  if ((size_t)p.B * p.H_kv * n_split > 0x7FFFFFFFull || p.B > 65535) return MPFA_ERR_UNSUPPORTED;
+  if (!aligned(p.q_codes, 16) || !aligned(p.q_sf, 16) || !aligned(p.k_codes, 256) || !aligned(p.k_sf, 256) ||
+      !aligned(p.v_fp8, 256) || !aligned(p.delta, 256) || !aligned(p.part_o, 16))
+    return MPFA_ERR_ALIGNMENT;
+  int dev = 0;
+  mpfa_status rc = device_info(&dev, n_sm);
+  if (rc != MPFA_OK) return rc;
+  uint8_t *const base = reinterpret_cast<uint8_t *>(p.part_o);
+  p.part_ml = reinterpret_cast<float2 *>(base + ws.ml);
+  p.n_split = (int)n_split;
+  // Kernels that a small call does not need are not launched (each costs a few microseconds of host time and one to two of
+  // latency): no counter where every CTA gets at most one item, no merge where no request can have two partitions.
+  p.ticket = (size_t)p.B * p.H_kv * n_split > (size_t)*n_sm ? reinterpret_cast<unsigned int *>(base + ws.ticket) : nullptr;
+  if (slots) {
+    p.final_ml = reinterpret_cast<float2 *>(base + ws.final_ml);
+    p.logits = reinterpret_cast<float *>(base + ws.logits);
+  }
+  return MPFA_OK;
+}
+
+template <int MODE>
+static mpfa_status decode_launch(const DecodeParams &p, int n_sm, cudaStream_t s) {
+  const size_t items = (size_t)p.B * p.H_kv * p.n_split;
   const unsigned grid = (unsigned)(items < (size_t)n_sm ? items : (size_t)n_sm);   // one persistent CTA per SM
+  mpfa_status rc = MPFA_OK;
   void (*kern)(const DecodeParams) = nullptr;
-  switch (H_q / H_kv) {
-    case 1: kern = decode_split_kernel<1>, rc = allow_smem<decode_split_kernel<1>>(D_SMEM); break;
-    case 2: kern = decode_split_kernel<2>, rc = allow_smem<decode_split_kernel<2>>(D_SMEM); break;
-    case 3: kern = decode_split_kernel<3>, rc = allow_smem<decode_split_kernel<3>>(D_SMEM); break;
-    case 4: kern = decode_split_kernel<4>, rc = allow_smem<decode_split_kernel<4>>(D_SMEM); break;
-    case 5: kern = decode_split_kernel<5>, rc = allow_smem<decode_split_kernel<5>>(D_SMEM); break;
-    case 6: kern = decode_split_kernel<6>, rc = allow_smem<decode_split_kernel<6>>(D_SMEM); break;
-    case 7: kern = decode_split_kernel<7>, rc = allow_smem<decode_split_kernel<7>>(D_SMEM); break;
-    case 8: kern = decode_split_kernel<8>, rc = allow_smem<decode_split_kernel<8>>(D_SMEM); break;
+  switch (p.H_q / p.H_kv) {
+    case 1: kern = decode_split_kernel<1, MODE>, rc = allow_smem<decode_split_kernel<1, MODE>>(D_SMEM); break;
+    case 2: kern = decode_split_kernel<2, MODE>, rc = allow_smem<decode_split_kernel<2, MODE>>(D_SMEM); break;
+    case 3: kern = decode_split_kernel<3, MODE>, rc = allow_smem<decode_split_kernel<3, MODE>>(D_SMEM); break;
+    case 4: kern = decode_split_kernel<4, MODE>, rc = allow_smem<decode_split_kernel<4, MODE>>(D_SMEM); break;
+    case 5: kern = decode_split_kernel<5, MODE>, rc = allow_smem<decode_split_kernel<5, MODE>>(D_SMEM); break;
+    case 6: kern = decode_split_kernel<6, MODE>, rc = allow_smem<decode_split_kernel<6, MODE>>(D_SMEM); break;
+    case 7: kern = decode_split_kernel<7, MODE>, rc = allow_smem<decode_split_kernel<7, MODE>>(D_SMEM); break;
+    case 8: kern = decode_split_kernel<8, MODE>, rc = allow_smem<decode_split_kernel<8, MODE>>(D_SMEM); break;
     default: return MPFA_ERR_UNSUPPORTED;
   }
   if (rc != MPFA_OK) return rc;
-  // Kernels that a small call does not need are not launched (each costs a few microseconds of host time and one to two of
-  // latency): no counter where every CTA gets at most one item, no merge where no request can have two partitions.
-  p.ticket = items > (size_t)n_sm ? reinterpret_cast<unsigned int *>(static_cast<uint8_t *>(workspace) + ws.ticket) : nullptr;
   if (p.ticket) MPFA_CUDA_OK(launch(decode_prep_kernel, dim3(1), dim3(1), 0, s, p.ticket));
   MPFA_CUDA_OK(launch(kern, dim3(grid), dim3(D_THREADS), D_SMEM, s, p));
-  if (n_split > FEW_PARTS)
-    MPFA_CUDA_OK(launch(decode_merge_kernel, dim3(H_q, B), dim3(128), 0, s, p));
-  else if (n_split > 1)
-    MPFA_CUDA_OK(launch(decode_merge_few_kernel, dim3((unsigned)(((long long)B * H_q + 3) / 4)), dim3(128), 0, s, p));
+  if (p.n_split > FEW_PARTS)
+    MPFA_CUDA_OK(launch(decode_merge_kernel<MODE>, dim3(p.H_q, p.B), dim3(128), 0, s, p));
+  else if (p.n_split > 1)
+    MPFA_CUDA_OK(launch(decode_merge_few_kernel<MODE>, dim3((unsigned)(((long long)p.B * p.H_q + 3) / 4)), dim3(128), 0, s, p));
+  return MPFA_OK;
+}
+
+extern "C" mpfa_status mpfa_decode(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
+                                   int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *st, float v_scale,
+                                   float softmax_scale, void *out_bf16, float *out_f32, void *workspace,
+                                   size_t workspace_bytes, int32_t *device_status, void *stream) {
+  DecodeParams p;
+  mpfa_status rc = decode_params(q, kv, page_table, max_pages_per_req, seq_lens, st, v_scale, softmax_scale, out_bf16, out_f32, workspace,
+                                 device_status, &p);
+  int n_sm = 0;
+  if (rc == MPFA_OK) rc = decode_place(p, all_splits(max_pages_per_req), 0, workspace_bytes, &n_sm);
+  return rc == MPFA_OK ? decode_launch<ALL_KEYS>(p, n_sm, static_cast<cudaStream_t>(stream)) : rc;
+}
+
+constexpr int MAX_PAGES = 1 << 24;   // token indices of the calls below stay within 31 bits
+
+extern "C" mpfa_status mpfa_decode_window(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
+                                          int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *st, float v_scale, int window,
+                                          int sinks, float softmax_scale, void *out_bf16, float *out_f32, void *workspace,
+                                          size_t workspace_bytes, int32_t *device_status, void *stream) {
+  DecodeParams p;
+  mpfa_status rc = decode_params(q, kv, page_table, max_pages_per_req, seq_lens, st, v_scale, softmax_scale, out_bf16, out_f32, workspace,
+                                 device_status, &p);
+  if (rc != MPFA_OK) return rc;
+  if (window <= 0 || sinks < 0) return MPFA_ERR_INVALID_ARG;
+  if (max_pages_per_req > MAX_PAGES) return MPFA_ERR_UNSUPPORTED;
+  p.window = window;
+  p.sinks = sinks;
+  int n_sm = 0;
+  rc = decode_place(p, window_splits(max_pages_per_req, window, sinks), 0, workspace_bytes, &n_sm);
+  return rc == MPFA_OK ? decode_launch<WINDOW>(p, n_sm, static_cast<cudaStream_t>(stream)) : rc;
+}
+
+extern "C" mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
+                                           int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *st, float v_scale,
+                                           float softmax_scale, float *weights, int weights_stride, void *out_bf16, float *out_f32,
+                                           void *workspace, size_t workspace_bytes, int32_t *device_status, void *stream) {
+  DecodeParams p;
+  mpfa_status rc = decode_params(q, kv, page_table, max_pages_per_req, seq_lens, st, v_scale, softmax_scale, out_bf16, out_f32, workspace,
+                                 device_status, &p);
+  if (rc != MPFA_OK) return rc;
+  if (!weights) return MPFA_ERR_INVALID_ARG;
+  if (max_pages_per_req > MAX_PAGES || p.H_kv > 65535) return MPFA_ERR_UNSUPPORTED;
+  const int slots = max_pages_per_req * PAGE;
+  if (weights_stride < slots) return MPFA_ERR_INVALID_ARG;
+  if (!aligned(weights, 4)) return MPFA_ERR_ALIGNMENT;
+  int n_sm = 0;
+  rc = decode_place(p, all_splits(max_pages_per_req), (size_t)slots, workspace_bytes, &n_sm);
+  if (rc != MPFA_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  rc = decode_launch<WEIGHTS>(p, n_sm, s);
+  if (rc != MPFA_OK) return rc;
+  // a block for each chunk of keys where that is a few waves of blocks or less
+  const int chunks = (slots + W_KEYS - 1) / W_KEYS, some = (16 * n_sm - 1) / (p.B * p.H_kv) + 1;
+  MPFA_CUDA_OK(launch(decode_weights_kernel, dim3((unsigned)(chunks < some ? chunks : some), (unsigned)p.H_kv, (unsigned)p.B), dim3(W_KEYS / 4), 0, s,
+                      p, weights, (size_t)weights_stride));
   return MPFA_OK;
 }

@@ -181,6 +181,22 @@ __device__ __forceinline__ int last_key(const PrefillParams &p, const Tile &tl, 
   return p.causal ? min(n_kv - 1, (PAGED ? min(r_abs, n_q - 1) : r_abs) + (n_kv - n_q)) : n_kv - 1;
 }
 
+// Keys that a row of a WINDOW instance does not see although they lie before its last one: from `sinks` up to its own `low`.
+template <bool PAGED, bool WINDOW>
+__device__ __forceinline__ int low_key(const PrefillParams &p, const Tile &tl, int r_abs) {
+  if constexpr (!WINDOW) return 0;
+  const int n_kv = PAGED ? tl.nkv : p.N_kv, n_q = PAGED ? tl.nq : p.N_q;
+  return max(min(r_abs, n_q - 1) + (n_kv - n_q) - p.window + 1, 0);
+}
+template <bool WINDOW>
+__device__ __forceinline__ bool hidden(int key, int limit, int low, int sinks) {
+  return key > limit || (WINDOW && key < low && key >= sinks);
+}
+template <bool WINDOW>   // whether the block has a key that the row does not see
+__device__ __forceinline__ bool partly_hidden(int key0, int limit, int low, int sinks) {
+  return key0 + TILE - 1 > limit || (WINDOW && max(key0, sinks) < min(key0 + TILE, low));
+}
+
 __device__ __forceinline__ float exponent_unit(const PrefillParams &p, int b) {
   return __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
 }
@@ -193,7 +209,10 @@ __device__ __forceinline__ float exponent_unit(const PrefillParams &p, int b) {
 // 24.6; 131072 x 32 102.6 / 97.7.  Not causal: 32768 x 16 5.97 / 6.03 ms, 49152 x 8 6.67 / 6.70, 65536 x 8 11.90 / 11.83.  From pages the
 // second form is ahead at every length (chunks of 512 on 4120 to 15011 tokens 314 / 310 us, 16384 x 32 1764 / 1720).  Neither
 // result is explained beyond the compiler's schedules, which differ in every role: the rule is what was measured.
-template <bool PAGED, bool LONG, bool RUNS>
+//
+// WINDOW: a sliding window and sinks.  An item's list of blocks leaves out those between the sinks and the window of the tile's first
+// row; everything else is a matter of addresses and masks (struct Tile, hidden()).
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false>
 __global__ void __launch_bounds__(NTHREADS, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const PrefillParams p, const PagedSrc pg) {
@@ -250,7 +269,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   grid_dependency_wait();
   const bool ordered = PAGED && p.B > 1 && p.B * p.nq_tiles <= MAX_GROUPS;
   if (ordered)   // the row-sum ring is not in use yet
-    length_order(p, pg, reinterpret_cast<uint16_t *>(smem + OFF_L), reinterpret_cast<uint16_t *>(smem + OFF_ORDER), tid, NTHREADS);
+    length_order<WINDOW>(p, pg, reinterpret_cast<uint16_t *>(smem + OFF_L), reinterpret_cast<uint16_t *>(smem + OFF_ORDER), tid, NTHREADS);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -274,7 +293,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     // uniform registers); a single elected lane issues each copy.
     bool ok = true;
     uint32_t nk_armed = 0, nv_armed = 0, nq_armed = 0;
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const uint32_t qb = ti & 1;
       if (ti >= 2) ok = cx.wait(BAR_Q_EMPTY + qb, ((ti >> 1) - 1) & 1u);
       if (!ok) break;
@@ -290,10 +309,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       PageLookup look;
       for (int t = 0; t < tl.T && ok; ++t) {
         const uint32_t c = gb + t;
-        const int jb = tl.T - 1 - t;
+        const int jb = block_of<WINDOW>(tl, tl.T - 1 - t);
         const uint32_t ks = c % KST, vs = c % VST;
         int page_lo = 0, page_hi = 0;
-        if (PAGED) look.get(pg, p.status, tl.b, tl.nkv, t, jb, lane, page_lo, page_hi);
+        if (PAGED && WINDOW)
+          look.template get<true>(pg, p.status, tl.b, tl.nkv, t, tl.T - 1 - t, lane, page_lo, page_hi, &tl, tl.low, p.sinks);
+        else if (PAGED)
+          look.get(pg, p.status, tl.b, tl.nkv, t, jb, lane, page_lo, page_hi);
         if (c >= (uint32_t)KST) ok = cx.wait(BAR_K_EMPTY + ks, (c / KST - 1) & 1u);
         if (!ok) break;
         if (PAGED) {
@@ -363,7 +385,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint64_t d_sfq00 = smem_desc(sbase + OFF_SFQ, 0, 128, SWZ_NONE);
     const uint64_t d_sfk0 = smem_desc(sbase + OFF_SFK, 0, 128, SWZ_NONE);
     bool ok = true;
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const uint32_t qb = ti & 1;
       ok = cx.wait(BAR_Q_FULL + qb, (ti >> 1) & 1u);
       if (!ok) break;
@@ -402,7 +424,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     // ==== paged source: re-tile the K scales and un-swizzle Delta_S of every stage ====
     const int G = p.H_q / p.H_kv;
     bool ok = true;
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const int rsw = tl.hq % G;
       for (int t = 0; t < tl.T && ok; ++t) {
         const uint32_t c = gb + t;
@@ -432,7 +454,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint32_t id_fp8 = idesc_e4m3(128, 128, 0, 1);
     const uint64_t d_v0 = smem_desc(sbase + OFF_V, 16, 1024, SWZ_128B);
     bool ok = true;
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const int run = run_length<RUNS>(tl.T);
       int begin = 0;   // of the run
       for (int t = 0; t < tl.T && ok; ++t) {
@@ -462,17 +484,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     float *s_m = reinterpret_cast<float *>(smem + OFF_M);
     bool ok = true;
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
-      const int limit = last_key<PAGED>(p, tl, tl.row0 + row);
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
+      const int limit = last_key<PAGED>(p, tl, WINDOW ? min(tl.row0 + row, (PAGED ? tl.nq : p.N_q) - 1) : tl.row0 + row);
+      const int low = low_key<PAGED, WINDOW>(p, tl, tl.row0 + row);
       float m = -INFINITY;
       for (int t = 0; t < tl.T; ++t) {
         const uint32_t c = gb + t;
-        const int key0 = (tl.T - 1 - t) * TILE;
+        const int key0 = block_of<WINDOW>(tl, tl.T - 1 - t) * TILE;
         const uint32_t tS = tm + TM_S + (c & 1) * 128 + lane_off;
         if (!__all_sync(0xffffffffu, cx.wait(BAR_S_FULL + (c & 1), (c >> 1) & 1u))) { ok = false; break; }
         tc_fence_after();
         float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
-        bool ragged = key0 + TILE - 1 > limit;
+        bool ragged = partly_hidden<WINDOW>(key0, limit, low, p.sinks);
         if (!LONG) ragged = __any_sync(0xffffffffu, ragged);   // the stores below are the whole warp's
 #pragma unroll 1
         for (int c0 = 0; c0 < 128; c0 += 32) {
@@ -483,7 +506,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           if (ragged) {   // diagonal / ragged block only
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (key0 + c0 + i > limit) x[i] = 0xFF800000u;   // -inf
+              if (hidden<WINDOW>(key0 + c0 + i, limit, low, p.sinks)) x[i] = 0xFF800000u;   // -inf
             if (!LONG) tmem_st32(tS + c0, x);
           }
 #pragma unroll
@@ -510,16 +533,17 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint32_t tS = tm + TM_S + grp * 128 + lane_off, tP = tm + TM_P + grp * 32 + lane_off;
     bool ok = true;
     uint32_t n_used = 0;   // items so far with T > 0: only those go through the row-sum ring
-    for (; ok && walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; ok && walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const int TT = tl.T;
       if (TT == 0) continue;   // nothing to attend to: the epilogue writes zeros without waiting for this role
-      const int limit = last_key<PAGED>(p, tl, tl.row0 + row);
+      const int limit = last_key<PAGED>(p, tl, WINDOW ? min(tl.row0 + row, (PAGED ? tl.nq : p.N_q) - 1) : tl.row0 + row);
+      const int low = low_key<PAGED, WINDOW>(p, tl, tl.row0 + row);
       const float lam = exponent_unit(p, tl.b);
       float m_own = -INFINITY;   // running maximum after this group's previous block
       float l_own = 0.0f;        // sum of 448 P over this group's blocks, relative to m_own
       for (int t = (grp ^ (int)gb) & 1; t < TT; t += 2) {
         const uint32_t c = gb + t;
-        const int key0 = (TT - 1 - t) * TILE;
+        const int key0 = block_of<WINDOW>(tl, TT - 1 - t) * TILE;
         // both of the block's conditions in one vote: the maximum is there, P V of block c-2 has consumed the group's P_hat
         const uint32_t par_m = (c / MST) & 1u, par_pe = ((c >> 1) - 1) & 1u;
         const bool both = cx.probe(BAR_M_FULL + c % MST, par_m) & (c < 2 || cx.probe(BAR_P_EMPTY + grp, par_pe));
@@ -543,10 +567,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         pin32(s[0]), pin32(s[1]), pin32(s[2]), pin32(s[3]);
         tc_fence_before();
         warp_arrive(cx.bar(BAR_S_EMPTY + grp), lane);
-        if (LONG && key0 + TILE - 1 > limit) {
+        if (LONG && partly_hidden<WINDOW>(key0, limit, low, p.sinks)) {
 #pragma unroll
           for (int i = 0; i < 128; ++i)
-            if (key0 + i > limit) s[i >> 5][i & 31] = 0xFF800000u;
+            if (hidden<WINDOW>(key0 + i, limit, low, p.sinks)) s[i >> 5][i & 31] = 0xFF800000u;
         }
         uint32_t packed[2][16];
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -594,7 +618,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     bool ok = true;
     uint32_t n_used = 0;   // items so far with T > 0 (slot and phase of the row-sum ring)
     warp_arrive(cx.bar(BAR_O_READY), lane);
-    for (; walk.template next<PAGED>(p, pg, tl); gb += tl.T, ++ti) {
+    for (; walk.template next<PAGED, WINDOW>(p, pg, tl); gb += tl.T, ++ti) {
       const int TT = tl.T, r_abs = tl.row0 + row;
       const float lam = exponent_unit(p, tl.b);
       const bool past = PAGED && r_abs >= tl.nq;   // nobody reads these rows: they ask for no rescale
@@ -753,13 +777,10 @@ extern "C" mpfa_status mpfa_prefill(const mpfa_fp4_tensor *q, const mpfa_fp4_ten
                               device_status, stream);
 }
 
-extern "C" mpfa_status mpfa_prefill_variant(const mpfa_fp4_tensor *q, const mpfa_fp4_tensor *k, const uint8_t *v_fp8,
-                                            const void *delta_s_bf16, const mpfa_stats *st, float v_scale, int causal,
-                                            float softmax_scale, int variant, void *out_bf16, float *out_f32,
-                                            int32_t *device_status, void *stream) {
-  if (variant != 0 && variant != MPFA_VARIANT_COMP_ELEMENTWISE && variant != MPFA_VARIANT_PV_BF16 && variant != MPFA_VARIANT_PV_FP4)
-    return MPFA_ERR_INVALID_ARG;
-  const bool ew = variant == MPFA_VARIANT_COMP_ELEMENTWISE && delta_s_bf16 != nullptr;
+// What the calls on contiguous operands share: the arguments checked and put into the launch parameters, and the grid.
+static mpfa_status contiguous_params(const mpfa_fp4_tensor *q, const mpfa_fp4_tensor *k, const uint8_t *v_fp8, const void *delta_s_bf16,
+                                     const mpfa_stats *st, float v_scale, int causal, float softmax_scale, void *out_bf16, float *out_f32,
+                                     int32_t *device_status, PrefillParams *params, unsigned *grid) {
   if (!q || !k || !v_fp8 || !st || !out_bf16 || !device_status) return MPFA_ERR_INVALID_ARG;
   if (!q->codes || !q->sf || !k->codes || !k->sf || !st->q_gscale || !st->k_gscale) return MPFA_ERR_INVALID_ARG;
   if (q->B <= 0 || q->B != k->B || q->H <= 0 || k->H <= 0 || q->N <= 0 || k->N <= 0) return MPFA_ERR_INVALID_ARG;
@@ -776,7 +797,7 @@ extern "C" mpfa_status mpfa_prefill_variant(const mpfa_fp4_tensor *q, const mpfa
   int dev = 0, n_sm = 0;
   mpfa_status rc = device_info(&dev, &n_sm);
   if (rc != MPFA_OK) return rc;
-  PrefillParams p;
+  PrefillParams &p = *params;
   p.q_sf = q->sf;
   p.k_sf = k->sf;
   p.delta = static_cast<const __nv_bfloat16 *>(delta_s_bf16);
@@ -796,28 +817,74 @@ extern "C" mpfa_status mpfa_prefill_variant(const mpfa_fp4_tensor *q, const mpfa
   p.softmax_scale = softmax_scale;
   p.v_scale = v_scale;
   p.n_items = (int)n_cta;
-  const unsigned grid = (unsigned)(n_cta < (uint64_t)n_sm ? n_cta : (uint64_t)n_sm);   // one persistent CTA per SM
+  *grid = (unsigned)(n_cta < (uint64_t)n_sm ? n_cta : (uint64_t)n_sm);   // one persistent CTA per SM
+  return MPFA_OK;
+}
+
+struct ContiguousMaps {
+  CUtensorMap q, k, v;
+};
+static mpfa_status contiguous_maps(const mpfa_fp4_tensor *q, const mpfa_fp4_tensor *k, const uint8_t *v_fp8, const PrefillParams &p,
+                                   ContiguousMaps *m) {
+  EncodeTiledFn enc;
+  mpfa_status rc = get_encoder(&enc);
+  if (rc != MPFA_OK) return rc;
+  const uint64_t q_rows = (uint64_t)p.B * p.H_q * p.nq_tiles * TILE, k_rows = (uint64_t)p.B * p.H_kv * p.nk_tiles * TILE;
+  if ((rc = make_map(enc, &m->q, q->codes, q_rows, 64)) != MPFA_OK) return rc;
+  if ((rc = make_map(enc, &m->k, k->codes, k_rows, 64)) != MPFA_OK) return rc;
+  return make_map(enc, &m->v, v_fp8, k_rows, 128);
+}
+
+extern "C" mpfa_status mpfa_prefill_variant(const mpfa_fp4_tensor *q, const mpfa_fp4_tensor *k, const uint8_t *v_fp8,
+                                            const void *delta_s_bf16, const mpfa_stats *st, float v_scale, int causal,
+                                            float softmax_scale, int variant, void *out_bf16, float *out_f32,
+                                            int32_t *device_status, void *stream) {
+  if (variant != 0 && variant != MPFA_VARIANT_COMP_ELEMENTWISE && variant != MPFA_VARIANT_PV_BF16 && variant != MPFA_VARIANT_PV_FP4)
+    return MPFA_ERR_INVALID_ARG;
+  const bool ew = variant == MPFA_VARIANT_COMP_ELEMENTWISE && delta_s_bf16 != nullptr;
+  PrefillParams p;
+  unsigned grid = 0;
+  mpfa_status rc = contiguous_params(q, k, v_fp8, delta_s_bf16, st, v_scale, causal, softmax_scale, out_bf16, out_f32, device_status, &p, &grid);
+  if (rc != MPFA_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool other_pv = variant == MPFA_VARIANT_PV_BF16 || variant == MPFA_VARIANT_PV_FP4;
   if (g_arrangement == 1 && !other_pv) return launch_prefill_pair(q, k, v_fp8, p, ew, s);
   if (ew || other_pv) return launch_prefill_variant(q, k, v_fp8, p, variant, grid, s);
-  EncodeTiledFn enc;
-  rc = get_encoder(&enc);
-  if (rc != MPFA_OK) return rc;
-  CUtensorMap tq, tk, tv;
-  if ((rc = make_map(enc, &tq, q->codes, q_rows, 64)) != MPFA_OK) return rc;
-  if ((rc = make_map(enc, &tk, k->codes, k_rows, 64)) != MPFA_OK) return rc;
-  if ((rc = make_map(enc, &tv, v_fp8, k_rows, 128)) != MPFA_OK) return rc;
-  if (nk_tiles < RUN_BLOCKS) return start<prefill_kernel<false, false, false>, SMEM_BYTES<false, false>>(grid, NTHREADS, s, tq, tk, tv, p, PagedSrc{});
-  if (k->N <= LONG_KEYS) return start<prefill_kernel<false, false, true>, SMEM_BYTES<false, true>>(grid, NTHREADS, s, tq, tk, tv, p, PagedSrc{});
-  return start<prefill_kernel<false, true, true>, SMEM_BYTES<false, true>>(grid, NTHREADS, s, tq, tk, tv, p, PagedSrc{});
+  ContiguousMaps m;
+  if ((rc = contiguous_maps(q, k, v_fp8, p, &m)) != MPFA_OK) return rc;
+  if (p.nk_tiles < RUN_BLOCKS) return start<prefill_kernel<false, false, false>, SMEM_BYTES<false, false>>(grid, NTHREADS, s, m.q, m.k, m.v, p, PagedSrc{});
+  if (k->N <= LONG_KEYS) return start<prefill_kernel<false, false, true>, SMEM_BYTES<false, true>>(grid, NTHREADS, s, m.q, m.k, m.v, p, PagedSrc{});
+  return start<prefill_kernel<false, true, true>, SMEM_BYTES<false, true>>(grid, NTHREADS, s, m.q, m.k, m.v, p, PagedSrc{});
 }
 
-extern "C" mpfa_status mpfa_prefill_paged(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
-                                          int max_pages_per_req, const int32_t *seq_lens, const int32_t *q_lens,
-                                          const mpfa_stats *st,
-                                          float v_scale, float softmax_scale, void *out_bf16, float *out_f32,
-                                          int32_t *device_status, void *stream) {
+// Most blocks that an item of 128 query rows can have under a window: its rows' windows cover window + 127 keys in a row.
+static int64_t window_blocks(int64_t n_blocks, int window, int sinks) {
+  const int64_t some = ((int64_t)sinks + TILE - 1) / TILE + ((int64_t)window + 2 * TILE - 3) / TILE + 1;
+  return some < n_blocks ? some : n_blocks;
+}
+
+extern "C" mpfa_status mpfa_prefill_window(const mpfa_fp4_tensor *q, const mpfa_fp4_tensor *k, const uint8_t *v_fp8,
+                                           const void *delta_s_bf16, const mpfa_stats *st, float v_scale, int window, int sinks,
+                                           float softmax_scale, void *out_bf16, float *out_f32, int32_t *device_status, void *stream) {
+  PrefillParams p;
+  unsigned grid = 0;
+  if (window <= 0 || sinks < 0) return MPFA_ERR_INVALID_ARG;
+  mpfa_status rc = contiguous_params(q, k, v_fp8, delta_s_bf16, st, v_scale, 1, softmax_scale, out_bf16, out_f32, device_status, &p, &grid);
+  if (rc != MPFA_OK) return rc;
+  p.window = window < p.N_kv ? window : p.N_kv;   // a wider one shows nothing more, and positions less it stay within 31 bits
+  p.sinks = sinks;
+  ContiguousMaps m;
+  if ((rc = contiguous_maps(q, k, v_fp8, p, &m)) != MPFA_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (window_blocks(p.nk_tiles, p.window, sinks) < RUN_BLOCKS)
+    return start<prefill_kernel<false, false, false, true>, SMEM_BYTES<false, false>>(grid, NTHREADS, s, m.q, m.k, m.v, p, PagedSrc{});
+  return start<prefill_kernel<false, false, true, true>, SMEM_BYTES<false, true>>(grid, NTHREADS, s, m.q, m.k, m.v, p, PagedSrc{});
+}
+
+// What the calls on pages share: the arguments checked and put into the launch parameters, and the grid.
+static mpfa_status paged_params(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table, int max_pages_per_req,
+                                const int32_t *seq_lens, const int32_t *q_lens, const mpfa_stats *st, float v_scale, float softmax_scale,
+                                void *out_bf16, float *out_f32, int32_t *device_status, PrefillParams *params, PagedSrc *source, unsigned *grid) {
   if (!q || !kv || !page_table || !seq_lens || !st || !out_bf16 || !device_status) return MPFA_ERR_INVALID_ARG;
   if (!q->codes || !q->sf || !kv->k_codes || !kv->k_sf || !kv->v_fp8 || !st->q_gscale || !st->k_gscale)
     return MPFA_ERR_INVALID_ARG;
@@ -835,7 +902,7 @@ extern "C" mpfa_status mpfa_prefill_paged(const mpfa_fp4_tensor *q, const mpfa_p
   int dev = 0, n_sm = 0;
   mpfa_status rc = device_info(&dev, &n_sm);
   if (rc != MPFA_OK) return rc;
-  PrefillParams p;
+  PrefillParams &p = *params;
   p.q_sf = q->sf;
   p.k_sf = nullptr;
   p.delta = static_cast<const __nv_bfloat16 *>(kv->delta_s_bf16);   // the kernel only tests it against null
@@ -855,7 +922,7 @@ extern "C" mpfa_status mpfa_prefill_paged(const mpfa_fp4_tensor *q, const mpfa_p
   p.softmax_scale = softmax_scale;
   p.v_scale = v_scale;
   p.n_items = (int)n_cta;
-  PagedSrc pg;
+  PagedSrc &pg = *source;
   pg.k_codes = kv->k_codes;
   pg.k_sf = kv->k_sf;
   pg.v_fp8 = kv->v_fp8;
@@ -865,14 +932,53 @@ extern "C" mpfa_status mpfa_prefill_paged(const mpfa_fp4_tensor *q, const mpfa_p
   pg.q_lens = q_lens;
   pg.max_pages = max_pages_per_req;
   pg.num_pages = kv->num_pages;
-  if (g_arrangement == 1) return launch_prefill_pair_paged(q, p, pg, static_cast<cudaStream_t>(stream));
+  *grid = (unsigned)(n_cta < (uint64_t)n_sm ? n_cta : (uint64_t)n_sm);
+  return MPFA_OK;
+}
+
+static mpfa_status query_map(const mpfa_fp4_tensor *q, const PrefillParams &p, CUtensorMap *map) {
   EncodeTiledFn enc;
-  rc = get_encoder(&enc);
+  const mpfa_status rc = get_encoder(&enc);
+  return rc != MPFA_OK ? rc : make_map(enc, map, q->codes, (uint64_t)p.B * p.H_q * p.nq_tiles * TILE, 64);
+}
+
+extern "C" mpfa_status mpfa_prefill_paged(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
+                                          int max_pages_per_req, const int32_t *seq_lens, const int32_t *q_lens,
+                                          const mpfa_stats *st,
+                                          float v_scale, float softmax_scale, void *out_bf16, float *out_f32,
+                                          int32_t *device_status, void *stream) {
+  PrefillParams p;
+  PagedSrc pg;
+  unsigned grid = 0;
+  mpfa_status rc = paged_params(q, kv, page_table, max_pages_per_req, seq_lens, q_lens, st, v_scale, softmax_scale, out_bf16, out_f32,
+                                device_status, &p, &pg, &grid);
   if (rc != MPFA_OK) return rc;
+  if (g_arrangement == 1) return launch_prefill_pair_paged(q, p, pg, static_cast<cudaStream_t>(stream));
   CUtensorMap tq;
-  if ((rc = make_map(enc, &tq, q->codes, q_rows, 64)) != MPFA_OK) return rc;
-  const unsigned grid = (unsigned)(n_cta < (uint64_t)n_sm ? n_cta : (uint64_t)n_sm);
+  if ((rc = query_map(q, p, &tq)) != MPFA_OK) return rc;
   if (max_pages_per_req < RUN_BLOCKS * (TILE / PAGE) - 1)   // no request can have RUN_BLOCKS blocks
     return start<prefill_kernel<true, true, false>, SMEM_BYTES<true, false>>(grid, NTHREADS, static_cast<cudaStream_t>(stream), tq, tq, tq, p, pg);
   return start<prefill_kernel<true, true, true>, SMEM_BYTES<true, true>>(grid, NTHREADS, static_cast<cudaStream_t>(stream), tq, tq, tq, p, pg);
+}
+
+extern "C" mpfa_status mpfa_prefill_paged_window(const mpfa_fp4_tensor *q, const mpfa_paged_kv *kv, const int32_t *page_table,
+                                                 int max_pages_per_req, const int32_t *seq_lens, const int32_t *q_lens,
+                                                 const mpfa_stats *st, float v_scale, int window, int sinks, float softmax_scale,
+                                                 void *out_bf16, float *out_f32, int32_t *device_status, void *stream) {
+  PrefillParams p;
+  PagedSrc pg;
+  unsigned grid = 0;
+  if (window <= 0 || sinks < 0) return MPFA_ERR_INVALID_ARG;
+  mpfa_status rc = paged_params(q, kv, page_table, max_pages_per_req, seq_lens, q_lens, st, v_scale, softmax_scale, out_bf16, out_f32,
+                                device_status, &p, &pg, &grid);
+  if (rc != MPFA_OK) return rc;
+  if (max_pages_per_req > (1 << 24)) return MPFA_ERR_UNSUPPORTED;   // token indices stay within 31 bits
+  p.window = window < max_pages_per_req * PAGE ? window : max_pages_per_req * PAGE;
+  p.sinks = sinks;
+  CUtensorMap tq;
+  if ((rc = query_map(q, p, &tq)) != MPFA_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (window_blocks((max_pages_per_req + 1) / 2, p.window, sinks) < RUN_BLOCKS)
+    return start<prefill_kernel<true, true, false, true>, SMEM_BYTES<true, false>>(grid, NTHREADS, s, tq, tq, tq, p, pg);
+  return start<prefill_kernel<true, true, true, true>, SMEM_BYTES<true, true>>(grid, NTHREADS, s, tq, tq, tq, p, pg);
 }

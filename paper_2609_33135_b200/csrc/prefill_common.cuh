@@ -22,6 +22,7 @@ struct PrefillParams {
   int B, N_q, N_kv, H_q, H_kv, nq_tiles, nk_tiles, n_items;
   int causal;
   float softmax_scale, v_scale;
+  int window = 0, sinks = 0;   // WINDOW instances: key j is visible to position p when j <= p and (j > p - window or j < sinks)
 };
 
 // K, V and Delta_S read from the paged cache instead of contiguous tensors: 64-token pages whose
@@ -146,15 +147,26 @@ struct Ctx {
 // the warp reads 32 page ids with one coalesced load (lane l: page index 2 jb + 1 - l); in between the ids come
 // from the lanes' registers.  A page past the end of the context (all its keys are masked) or with an id outside
 // the pool (reported in *status) is replaced by the block's other page, so operand tiles always hold finite bytes.
+struct Tile;
+template <bool WINDOW>
+__device__ __forceinline__ int block_of(const Tile &t, int v);
 struct PageLookup {
   int ids;
+  // WINDOW: a page without a key that some row of the tile sees counts as one past the end, so its table entry is not looked at.
+  template <bool WINDOW = false>
   __device__ __forceinline__ void get(const PagedSrc &pg, int32_t *status, int b, int nkv, int t, int jb, int lane,
-                                      int &page_lo, int &page_hi) {
+                                      int &page_lo, int &page_hi, const Tile *tl = nullptr, int low = 0, int sinks = 0) {
     if ((t & 15) == 0) {
       const int n_pg = (nkv + 63) >> 6;
-      const int pi = 2 * jb + 1 - lane;
+      int pi = 2 * jb + 1 - lane;
+      bool in = pi >= 0 && pi < n_pg;
+      if constexpr (WINDOW) {   // jb: the block's number in the item's list, which lane l looks l / 2 blocks ahead in
+        const int v = jb - (lane >> 1);
+        pi = 2 * block_of<true>(*tl, max(v, 0)) + 1 - (lane & 1);
+        in = v >= 0 && pi < n_pg && (pi * 64 + 63 >= low || pi * 64 < sinks);
+      }
       int id = -1;
-      if (pi >= 0 && pi < n_pg) {
+      if (in) {
         id = pg.page_table[(size_t)b * pg.max_pages + pi];
         if (id < 0 || id >= pg.num_pages) {
           atomicOr(status, MPFA_DEV_BAD_PAGE);
@@ -178,10 +190,17 @@ constexpr int MAX_GROUPS = 512;   // (query tile, request) groups that are order
 struct Tile {
   int b, hq, hk, qt, row0, T;   // T: KV blocks to visit
   int nkv, nq;                  // keys and queries of this item's request
+  // WINDOW: first key that the window of the tile's first row reaches; the list of blocks is [0, heads), the sinks', and from
+  // heads + shift on, the window's (0 and 0 where nothing lies between)
+  int low, heads, shift;
 };
 
+// The v-th block of an item's list (ascending).
+template <bool WINDOW>
+__device__ __forceinline__ int block_of(const Tile &t, int v) { return WINDOW && v >= t.heads ? v + t.shift : v; }
+
 // Lengths of the item at t.b, t.row0.
-template <bool PAGED>
+template <bool PAGED, bool WINDOW = false>
 __device__ __forceinline__ void geometry(const PrefillParams &pp, const PagedSrc &pg, Tile &t) {
   const int n_q = (PAGED && pg.q_lens) ? min(pg.q_lens[t.b], pp.N_q) : pp.N_q;
   const int last_row = min(n_q - 1, t.row0 + TILE - 1);
@@ -191,6 +210,13 @@ __device__ __forceinline__ void geometry(const PrefillParams &pp, const PagedSrc
   t.nq = n_q;
   const int last_key = pp.causal ? min(n_kv - 1, last_row + (n_kv - n_q)) : n_kv - 1;   // bottom-right aligned
   t.T = (last_key < 0 || (PAGED && t.row0 >= n_q)) ? 0 : last_key / TILE + 1;
+  if constexpr (WINDOW) {
+    t.low = max(t.row0 + (n_kv - n_q) - pp.window + 1, 0);
+    t.heads = (min(pp.sinks, t.low) + TILE - 1) / TILE;
+    t.shift = t.low / TILE - t.heads;
+    if (t.shift <= 0) t.heads = t.shift = 0;
+    if (t.T > 0) t.T -= t.shift;
+  }
 }
 
 // The list of work items of this CTA.  Items are ordered by length (latest query tile first; all heads of a
@@ -204,7 +230,7 @@ struct TileWalk {
   int round;   // everything else is read from the kernel parameters (constant bank), not kept in registers
   const uint16_t *order;   // paged source: groups by descending length; null: as numbered
   __device__ __forceinline__ void init(const uint16_t *o) { round = 0, order = o; }
-  template <bool PAGED>
+  template <bool PAGED, bool WINDOW = false>
   __device__ __forceinline__ bool next(const PrefillParams &pp, const PagedSrc &pg, Tile &t) {
     const int c = (round & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x;
     const int i = round * (int)gridDim.x + c;
@@ -217,20 +243,21 @@ struct TileWalk {
     t.hq = i % pp.H_q;
     t.hk = t.hq / (pp.H_q / pp.H_kv);
     t.row0 = t.qt * TILE;
-    geometry<PAGED>(pp, pg, t);
+    geometry<PAGED, WINDOW>(pp, pg, t);
     return true;
   }
 };
 
 // Work items of a paged batch by descending length: ranks of the (query tile, request) groups by counting.  lengths, order:
 // MAX_GROUPS entries each; called by the whole CTA, which synchronises before order is read.
+template <bool WINDOW = false>
 __device__ __forceinline__ void length_order(const PrefillParams &pp, const PagedSrc &pg, uint16_t *lengths, uint16_t *order, int tid, int n_threads) {
   const int n = pp.nq_tiles * pp.B;
   for (int g = tid; g < n; g += n_threads) {
     Tile t;
     t.b = g % pp.B;
     t.row0 = (pp.nq_tiles - 1 - g / pp.B) * TILE;
-    geometry<true>(pp, pg, t);
+    geometry<true, WINDOW>(pp, pg, t);
     lengths[g] = (uint16_t)min(t.T, 65535);
   }
   __syncthreads();
