@@ -1,12 +1,13 @@
 // Eviction from the paged cache by accumulated attention weight, for sm_100a: two kernels, neither with any arithmetic on the tokens.
 //
 // evict_select_kernel, one CTA per (request, kv head).  Of n > keep tokens the first `sinks` and the last `recent` stay; of the others
-// the need = keep - sinks - recent of largest weight, equal ones by slot.  Weights are ordered as the 32-bit integers that compare like
-// them (-0 as +0, NaN below everything).  The need-th largest is found digit by digit (11, 11, 10 bits): a histogram of the candidates
-// that agree with the digits so far, and the bin in which the count from above reaches what is still needed.  Then one ordered pass
-// over the slots writes those above the value found, and the lowest slots of those equal to it.  Histograms are integer counts, so the
-// order of the atomics does not show.  One read of the weights from memory: the passes after the first find them in shared memory, or
-// in L2 where there are more than fit.
+// the need = keep - sinks - recent with the largest 64-bit keys: the weight as the 32-bit integer that compares like it (-0 as +0, NaN
+// below everything), then the slot, lower ones larger.  No two keys are equal, so what is kept is what is not below the need-th largest.
+// It is found by digits of 12 bits from the top: a histogram of the candidates that agree with the digits so far, and the bin in which the
+// count from above reaches what is still needed.  As soon as that bin holds few enough they are listed and ranked against one another,
+// one to a thread; with weights that differ that is after the first digit.  Histograms are integer counts and the list's order decides
+// nothing, so the order of the atomics does not show.  One read of the weights from memory: what comes after finds them in shared memory,
+// or in L2 where there are more than fit.
 //
 // evict_move_kernel, one CTA per (new page, kv head, request): the 64 tokens of the page from their slots.  A token's K codes, scales,
 // V and Delta_S entries are whole 16-, 8- and 2-byte pieces in every slot, whose places depend on the slot (include/mpfa.h), so the new
@@ -33,8 +34,10 @@ struct EvictParams {
 };
 
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
-constexpr int DIGIT = 11, BINS = 1 << DIGIT;
+constexpr int DIGIT = 12, BINS = 1 << DIGIT;
+constexpr int LIST = 256;          // ranking m candidates against one another takes about m^2 / 32 cycles, a digit 2500
 constexpr int SEL_CACHE = 49152;   // weights held in shared memory between the passes: 192 KB
+constexpr int SEL_AHEAD = 8;       // loads of a thread on the way
 
 __device__ __forceinline__ uint32_t order_of(float w) {
   if (w != w) return 0u;
@@ -42,37 +45,117 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum over the block in thread order, and the total.  tmp: SEL_WARPS + 1 words.
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *tmp, uint32_t &total) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t incl = x;
+// Exclusive sum over the block in thread order.  tmp: SEL_WARPS words, not written again before the block's next barrier.
+__device__ __forceinline__ uint32_t warp_scan(uint32_t x) {
+  const int lane = threadIdx.x & 31;
+  uint32_t s = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
+    const uint32_t a = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += a;
   }
-  __syncthreads();   // tmp of the scan before has been read
-  if (lane == 31) tmp[warp] = incl;
+  return s - x;
+}
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *tmp) {
+  static_assert(SEL_WARPS == 32, "a lane for each warp");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t mine = warp_scan(x);
+  if (lane == 31) tmp[warp] = mine + x;
   __syncthreads();
-  if (warp == 0) {
-    const uint32_t mine = tmp[lane];
-    uint32_t s = mine;
+  return mine + __shfl_sync(0xffffffffu, warp_scan(tmp[lane]), warp);   // every warp adds up the warps before it
+}
+
+struct SelectShared {
+  union {
+    uint32_t hist[BINS];
+    uint64_t list[LIST];
+  };
+  uint32_t tmp[2][SEL_WARPS], bin, need, inside, listed;
+  uint64_t border;
+};
+
+__device__ __forceinline__ uint64_t key_of(float w, int slot) { return (uint64_t)order_of(w) << 32 | (0xffffffffu - (uint32_t)slot); }
+
+// The slots kept of n > keep, to kept[] in ascending order.  w: shared or global memory.
+template <bool SHARED>
+__device__ __forceinline__ void select_tokens(const EvictParams &p, const float *w, int n, int32_t *kept, SelectShared &sh) {
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int first = p.sinks, last = n - p.recent;   // the candidates: [first, last)
+  uint32_t need = (uint32_t)(p.keep - p.sinks - p.recent);
+  uint64_t border = ~0ull;   // no key is as large
+  if (need > 0) {
+    uint64_t value = 0, mask = 0;
+    int shift = 64;
+#pragma unroll 1
+    for (uint32_t inside = (uint32_t)(last - first); inside > LIST;) {
+      const int bits = min(DIGIT, shift);
+      shift -= bits;
+      __syncthreads();   // of the pass before: bin, need, inside and the histogram have been read
+      for (int i = t; i < BINS; i += SEL_THREADS) sh.hist[i] = 0;
+      __syncthreads();
+#pragma unroll 4
+      for (int i = first + t; i < last; i += SEL_THREADS) {
+        const uint64_t k = key_of(w[i], i);
+        if ((k & mask) == value) atomicAdd(&sh.hist[(uint32_t)(k >> shift) & ((1u << bits) - 1u)], 1u);
+      }
+      __syncthreads();
+      // a run of bins to a thread, the highest first: the bin in which the count from above reaches `need`
+      constexpr int PER = BINS / SEL_THREADS;
+      const int top = BINS - 1 - PER * t;
+      uint32_t c[PER], sum = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += v;
+      for (int u = 0; u < PER; ++u) c[u] = sh.hist[top - u], sum += c[u];
+      uint32_t above = block_scan(sum, sh.tmp[0]);
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        if (above < need && need <= above + c[u]) sh.bin = (uint32_t)(top - u), sh.need = need - above, sh.inside = c[u];
+        above += c[u];
+      }
+      __syncthreads();
+      value |= (uint64_t)sh.bin << shift;
+      mask |= (uint64_t)((1u << bits) - 1u) << shift;
+      need = sh.need, inside = sh.inside;
     }
-    tmp[lane] = s - mine;
-    if (lane == 31) tmp[SEL_WARPS] = s;
+    // the candidates of that bin, in any order; the one with need - 1 larger ones is the border
+    __syncthreads();
+    if (t == 0) sh.listed = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = first + t; i < last; i += SEL_THREADS) {
+      const uint64_t k = key_of(w[i], i);
+      if ((k & mask) == value) sh.list[atomicAdd(&sh.listed, 1u)] = k;
+    }
+    __syncthreads();
+    const int m = (int)sh.listed;
+    if (t < m) {
+      const uint64_t mine = sh.list[t];
+      uint32_t larger = 0;
+#pragma unroll 8
+      for (int i = 0; i < m; ++i) larger += sh.list[i] > mine ? 1u : 0u;
+      if (larger == need - 1) sh.border = mine;
+    }
+    __syncthreads();
+    border = sh.border;
   }
-  __syncthreads();
-  total = tmp[SEL_WARPS];
-  return tmp[warp] + incl - x;
+  // In the order of the slots: each warp takes a run of them, counts, and writes when it knows what the warps before it have.
+  const int run = ((n + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, begin = min(warp * run, n), end = min(begin + run, n);
+  auto stays = [&](int i) { return i < end && (i < first || i >= last || key_of(w[i], i) >= border); };
+  uint32_t count = 0;
+#pragma unroll 4
+  for (int i0 = begin; i0 < end; i0 += 32) count += stays(i0 + lane) ? 1u : 0u;
+  uint32_t to = __shfl_sync(0xffffffffu, block_scan(count, sh.tmp[1]), 0);
+#pragma unroll 4
+  for (int i0 = begin; i0 < end; i0 += 32) {
+    const bool s = stays(i0 + lane);
+    const uint32_t bits = __ballot_sync(0xffffffffu, s);
+    if (s) kept[to + __popc(bits & ((1u << lane) - 1u))] = i0 + lane;
+    to += __popc(bits);
+  }
 }
 
 __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t held[];          // the order of each slot's weight, where they fit
-  __shared__ uint32_t hist[BINS], tmp[SEL_WARPS + 1], found[2];
+  extern __shared__ float held[];             // the weights, where they fit
+  __shared__ SelectShared sh;
   grid_dependency_wait();
   launch_dependents();
   const int hk = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
@@ -80,136 +163,107 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
   const float *const w = p.weights + head * p.weights_stride;
   int32_t *const kept = p.kept + head * p.keep;
   float *const out = p.new_weights + head * p.new_stride;
+  // the first weights are requested before the length is known: their slots exist whatever it is
+  const int most = p.max_pages * PAGE;
+  float x[SEL_AHEAD];
+#pragma unroll
+  for (int u = 0; u < SEL_AHEAD; ++u) x[u] = t + u * SEL_THREADS < most ? w[t + u * SEL_THREADS] : 0.0f;
   const int n = p.length(b), count = min(n, p.keep);
   if (hk == 0 && t == 0) p.new_lens[b] = count;
   for (size_t i = (size_t)count + t; i < p.new_stride; i += SEL_THREADS) out[i] = 0.0f;
   for (int i = count + t; i < p.keep; i += SEL_THREADS) kept[i] = -1;
   if (n <= p.keep) {
-    for (int i = t; i < n; i += SEL_THREADS) kept[i] = i, out[i] = w[i];
-    return;
-  }
-  const int first = p.sinks, last = n - p.recent;   // the candidates: [first, last)
-  const bool fits = n <= SEL_CACHE;
-  if (fits)
-    for (int i = t; i < n; i += SEL_THREADS) held[i] = order_of(w[i]);
-  uint32_t need = (uint32_t)(p.keep - p.sinks - p.recent), value = 0, mask = 0;
-  if (need > 0) {
-    int shift = 32;
-#pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-      const int bits = pass < 2 ? DIGIT : 32 - 2 * DIGIT;
-      shift -= bits;
-      __syncthreads();
-      for (int i = t; i < BINS; i += SEL_THREADS) hist[i] = 0;
-      __syncthreads();
-      for (int i = first + t; i < last; i += SEL_THREADS) {
-        const uint32_t u = fits ? held[i] : order_of(w[i]);
-        if ((u & mask) == value) atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1u)], 1u);
-      }
-      __syncthreads();
-      // two bins to a thread, the highest first: the bin in which the count from above reaches `need`
-      const int hi = BINS - 1 - 2 * t;
-      const uint32_t a = hist[hi], c = hist[hi - 1];
-      uint32_t total;
-      const uint32_t above = block_scan(a + c, tmp, total);
-      if (above < need && need <= above + a + c) {
-        const bool second = need > above + a;
-        found[0] = (uint32_t)(second ? hi - 1 : hi);
-        found[1] = need - above - (second ? a : 0u);   // how many of that bin
-      }
-      __syncthreads();
-      value |= found[0] << shift;
-      mask |= ((1u << bits) - 1u) << shift;
-      need = found[1];
+    for (int i = t; i < n; i += SEL_THREADS) kept[i] = i;
+  } else if (n <= SEL_CACHE) {
+#pragma unroll
+    for (int u = 0; u < SEL_AHEAD; ++u)
+      if (t + u * SEL_THREADS < n) held[t + u * SEL_THREADS] = x[u];
+    for (int i = t + SEL_AHEAD * SEL_THREADS; i < n; i += SEL_AHEAD * SEL_THREADS) {
+#pragma unroll
+      for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i + u * SEL_THREADS < n ? w[i + u * SEL_THREADS] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < SEL_AHEAD; ++u)
+        if (i + u * SEL_THREADS < n) held[i + u * SEL_THREADS] = x[u];
     }
+    __syncthreads();
+    select_tokens<true>(p, held, n, kept, sh);
   } else {
-    value = 0xffffffffu;
-  }
-  // All candidates above `value` and the first `need` of those equal to it, in the order of the slots.
-  __syncthreads();
-  uint32_t at = 0, equal = 0;   // written, and equal ones met, so far
-#pragma unroll 1
-  for (int i0 = 0; i0 < n; i0 += SEL_THREADS) {
-    const int i = i0 + t;
-    const bool in = i < n, candidate = in && i >= first && i < last;
-    float x = 0.0f;
-    uint32_t u = 0;
-    if (in) x = w[i], u = candidate ? (fits ? held[i] : order_of(x)) : 0u;
-    const bool eq = candidate && u == value && p.keep > p.sinks + p.recent;
-    const bool sure = in && (!candidate || u > value);
-    // both counts in one scan: at most 1024 each
-    uint32_t total;
-    const uint32_t before = block_scan((sure ? 1u : 0u) | (eq ? 0x10000u : 0u), tmp, total);
-    const uint32_t eq_before = equal + (before >> 16);
-    const bool take = sure || (eq && eq_before < need);
-    // of the equal ones before this slot, those that were taken count
-    const uint32_t eq_taken = min(eq_before, need) - min(equal, need);
-    if (take) {
-      const uint32_t to = at + (before & 0xffffu) + eq_taken;
-      kept[to] = i;
-      out[to] = x;
-    }
-    const uint32_t eq_total = total >> 16;
-    at += (total & 0xffffu) + min(equal + eq_total, need) - min(equal, need);
-    equal += eq_total;
+    select_tokens<false>(p, w, n, kept, sh);
   }
 }
 
+// A warp takes eight tokens of a new page: their V is 64 pieces of 16 bytes, their K codes 32, and their Delta_S 16 bytes of each head's
+// row there.  Everything is read before anything is written.
 constexpr int MOVE_THREADS = 256;
-__global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const __grid_constant__ EvictParams p) {
-  __shared__ int64_t slab[PAGE];   // (page, kv head) slab that a token comes from, -1: none
-  __shared__ int slot[PAGE];
-  const int page = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x;
+__global__ void __launch_bounds__(MOVE_THREADS, 8) evict_move_kernel(const __grid_constant__ EvictParams p) {
+  const int page = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dependency_wait();
+  const int at = page * PAGE + warp * 8 + (lane & 7);   // lane l: token l mod 8
+  const int to = p.new_table[(size_t)b * p.new_pages + page];
+  const int from = at < p.keep ? p.kept[((size_t)b * p.H_kv + hk) * p.keep + at] : -1;   // -1 past the last token
   const int count = min(p.length(b), p.keep);
   if (page * PAGE >= count) return;
-  const int to = p.new_table[(size_t)b * p.new_pages + page];
+  if (from >= 0 && lane < 8) {
+    const size_t head = (size_t)b * p.H_kv + hk;
+    p.new_weights[head * p.new_stride + at] = p.weights[head * p.weights_stride + from];
+  }
   if (to < 0 || to >= p.num_pages) {
-    if (t == 0) atomicOr(p.status, MPFA_DEV_BAD_PAGE);
+    if (threadIdx.x == 0) atomicOr(p.status, MPFA_DEV_BAD_PAGE);
     return;
   }
-  if (t < PAGE) {
-    int64_t s = -1;
-    int at = 0;
-    if (page * PAGE + t < count) {
-      at = p.kept[((size_t)b * p.H_kv + hk) * p.keep + page * PAGE + t];
-      const int from = p.page_table[(size_t)b * p.max_pages + at / PAGE];
-      if (from >= 0 && from < p.num_pages)
-        s = (int64_t)from * p.H_kv + hk;
-      else
-        atomicOr(p.status, MPFA_DEV_BAD_PAGE);
+  int id = -1;
+  if (from >= 0) {
+    id = p.page_table[(size_t)b * p.max_pages + from / PAGE];
+    if (id < 0 || id >= p.num_pages) {
+      id = -1;
+      atomicOr(p.status, MPFA_DEV_BAD_PAGE);
     }
-    slab[t] = s;
-    slot[t] = at % PAGE;
   }
-  __syncthreads();
-  const size_t dst = (size_t)to * p.H_kv + hk;
+  const int slot = from & (PAGE - 1);
+  const int G = p.H_q / p.H_kv;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  {   // K codes: four 16-byte pieces a token
-    const int i = t >> 2, c = t & 3, s = slot[i];
-    uint4 x = zero;
-    if (slab[i] >= 0) x = *reinterpret_cast<const uint4 *>(p.k_codes + slab[i] * 4096 + s * 64 + ((c ^ ((s & 7) >> 1)) << 4));
-    *reinterpret_cast<uint4 *>(p.k_codes + dst * 4096 + i * 64 + ((c ^ ((i & 7) >> 1)) << 4)) = x;
-  }
+  uint4 v[2] = {zero, zero}, k = zero;
+  uint2 sf = make_uint2(0u, 0u);
+  uint16_t d[2] = {0, 0};
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {   // V: eight
-    const int i = (t >> 3) + 32 * u, c = t & 7, s = slot[i];
-    uint4 x = zero;
-    if (slab[i] >= 0) x = *reinterpret_cast<const uint4 *>(p.v_fp8 + slab[i] * 8192 + s * 128 + ((c ^ (s & 7)) << 4));
-    *reinterpret_cast<uint4 *>(p.v_fp8 + dst * 8192 + i * 128 + ((c ^ (i & 7)) << 4)) = x;
+  for (int u = 0; u < 2; ++u) {
+    const int i = (lane >> 3) + 4 * u, c = lane & 7;
+    const int id_i = __shfl_sync(0xffffffffu, id, i), s = __shfl_sync(0xffffffffu, slot, i);
+    if (id_i >= 0) v[u] = *reinterpret_cast<const uint4 *>(p.v_fp8 + ((size_t)id_i * p.H_kv + hk) * 8192 + s * 128 + ((c ^ (s & 7)) << 4));
   }
-  if (t < PAGE) {
-    uint2 x = make_uint2(0u, 0u);
-    if (slab[t] >= 0) x = *reinterpret_cast<const uint2 *>(p.k_sf + slab[t] * 512 + slot[t] * 8);
-    *reinterpret_cast<uint2 *>(p.k_sf + dst * 512 + t * 8) = x;
+  {
+    const int i = lane >> 2, c = lane & 3;
+    const int id_i = __shfl_sync(0xffffffffu, id, i), s = __shfl_sync(0xffffffffu, slot, i);
+    if (id_i >= 0) k = *reinterpret_cast<const uint4 *>(p.k_codes + ((size_t)id_i * p.H_kv + hk) * 4096 + s * 64 + ((c ^ ((s & 7) >> 1)) << 4));
   }
+  if (id >= 0) {
+    const size_t slab = (size_t)id * p.H_kv + hk;
+    if (lane < 8) sf = *reinterpret_cast<const uint2 *>(p.k_sf + slab * 512 + slot * 8);
+    if (p.delta) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int g = (lane >> 3) + 4 * u;
+        if (g < G) d[u] = p.delta[(slab * G + g) * PAGE + (((slot >> 3) ^ g) << 3) + (slot & 7)];
+      }
+    }
+  }
+  const size_t dst = (size_t)to * p.H_kv + hk;
+  const int row = warp * 8;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = (lane >> 3) + 4 * u, c = lane & 7;
+    *reinterpret_cast<uint4 *>(p.v_fp8 + dst * 8192 + (row + i) * 128 + ((c ^ i) << 4)) = v[u];
+  }
+  {
+    const int i = lane >> 2, c = lane & 3;
+    *reinterpret_cast<uint4 *>(p.k_codes + dst * 4096 + (row + i) * 64 + ((c ^ (i >> 1)) << 4)) = k;
+  }
+  if (lane < 8) *reinterpret_cast<uint2 *>(p.k_sf + dst * 512 + (row + lane) * 8) = sf;
   if (p.delta) {
-    const int G = p.H_q / p.H_kv;
-    for (int k = t; k < G * PAGE; k += MOVE_THREADS) {
-      const int g = k / PAGE, i = k % PAGE, s = slot[i];
-      uint16_t x = 0;
-      if (slab[i] >= 0) x = p.delta[(slab[i] * G + g) * PAGE + (((s >> 3) ^ (g & 7)) << 3) + (s & 7)];
-      p.delta[(dst * G + g) * PAGE + (((i >> 3) ^ (g & 7)) << 3) + (i & 7)] = x;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int g = (lane >> 3) + 4 * u;
+      if (g < G) p.delta[(dst * G + g) * PAGE + ((warp ^ g) << 3) + (lane & 7)] = d[u];
     }
   }
 }

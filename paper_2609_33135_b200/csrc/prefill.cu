@@ -188,9 +188,10 @@ __device__ __forceinline__ int low_key(const PrefillParams &p, const Tile &tl, i
   const int n_kv = PAGED ? tl.nkv : p.N_kv, n_q = PAGED ? tl.nq : p.N_q;
   return max(min(r_abs, n_q - 1) + (n_kv - n_q) - p.window + 1, 0);
 }
-template <bool WINDOW>
-__device__ __forceinline__ bool hidden(int key, int limit, int low, int sinks) {
-  return key > limit || (WINDOW && key < low && key >= sinks);
+// Bit i: whether key + i is visible to a row of a WINDOW instance.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t visible32(int key, int limit, int low, int sinks) {
+  return first_bits(limit - key + 1) & (~first_bits(low - key) | first_bits(sinks - key));
 }
 template <bool WINDOW>   // whether the block has a key that the row does not see
 __device__ __forceinline__ bool partly_hidden(int key0, int limit, int low, int sinks) {
@@ -496,17 +497,28 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         tc_fence_after();
         float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
         bool ragged = partly_hidden<WINDOW>(key0, limit, low, p.sinks);
-        if (!LONG) ragged = __any_sync(0xffffffffu, ragged);   // the stores below are the whole warp's
+        if (!LONG || WINDOW) ragged = __any_sync(0xffffffffu, ragged);   // the stores below are the whole warp's
 #pragma unroll 1
         for (int c0 = 0; c0 < 128; c0 += 32) {
           uint32_t x[32];
           tmem_ld32(tS + c0, x);
           tmem_ld_wait();
           pin32(x);
-          if (ragged) {   // diagonal / ragged block only
+          if constexpr (WINDOW) {
+            if (ragged) {
+              // an item has up to five such blocks, at most two chunks of each mixed for a warp's rows: the others cost a vote
+              const uint32_t see = visible32(key0 + c0, limit, low, p.sinks);
+              if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!(see >> i & 1u)) x[i] = 0xFF800000u;
+                if (!LONG) tmem_st32(tS + c0, x);
+              }
+            }
+          } else if (ragged) {   // diagonal / ragged block only
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (hidden<WINDOW>(key0 + c0 + i, limit, low, p.sinks)) x[i] = 0xFF800000u;   // -inf
+              if (key0 + c0 + i > limit) x[i] = 0xFF800000u;   // -inf
             if (!LONG) tmem_st32(tS + c0, x);
           }
 #pragma unroll
@@ -567,10 +579,22 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         pin32(s[0]), pin32(s[1]), pin32(s[2]), pin32(s[3]);
         tc_fence_before();
         warp_arrive(cx.bar(BAR_S_EMPTY + grp), lane);
-        if (LONG && partly_hidden<WINDOW>(key0, limit, low, p.sinks)) {
+        if (LONG && (WINDOW ? __any_sync(0xffffffffu, partly_hidden<WINDOW>(key0, limit, low, p.sinks)) : key0 + TILE - 1 > limit)) {
+          if constexpr (WINDOW) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (hidden<WINDOW>(key0 + i, limit, low, p.sinks)) s[i >> 5][i & 31] = 0xFF800000u;
+            for (int c0 = 0; c0 < 4; ++c0) {
+              const uint32_t see = visible32(key0 + 32 * c0, limit, low, p.sinks);
+              if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!(see >> i & 1u)) s[c0][i] = 0xFF800000u;
+              }
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 128; ++i)
+              if (key0 + i > limit) s[i >> 5][i & 31] = 0xFF800000u;
+          }
         }
         uint32_t packed[2][16];
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
