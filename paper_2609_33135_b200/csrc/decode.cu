@@ -1082,29 +1082,52 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
 
 // What each key received: weights[b, kv head, j] += sum over the group's heads of 2^(lam (S_j - m)) / l, in FP32 from the logits that the
 // split kernel kept and the (m, l) of the whole request.  A thread takes four keys, a block chunks of 1024, heads in ascending order: one
-// writer per sum, a fixed order.  Bound by memory: 4 G bytes of logits per key read back (mostly from L2), 8 of the sum.
-constexpr int W_KEYS = 1024;
-__global__ void __launch_bounds__(W_KEYS / 4) decode_weights_kernel(const __grid_constant__ DecodeParams p, float *weights, size_t stride) {
+// writer per sum, a fixed order.  Bound by memory: 4 G bytes of logits per key read back, 8 of the sum; and at its beginning by three loads
+// that wait for one another (length, logits, and the merge's (m, l) beside them), which is why all heads' are asked for at once.
+constexpr int W_KEYS = 1024, W_THREADS = W_KEYS / 4;
+template <int G>
+__global__ void __launch_bounds__(W_THREADS) decode_weights_kernel(const __grid_constant__ DecodeParams p, float *weights, size_t stride) {
   grid_dependency_wait();
-  const int hk = blockIdx.y, b = blockIdx.z, G = p.H_q / p.H_kv;
-  const int L = p.length<WEIGHTS>(b);
+  const int hk = blockIdx.y, b = blockIdx.z;
   const size_t slots = (size_t)p.max_pages * PAGE, head0 = (size_t)b * p.H_q + (size_t)hk * G;
+  float2 ml[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) ml[g] = p.final_ml[head0 + g];
   const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
+  const int L = p.length<WEIGHTS>(b);
   float *const sum = weights + ((size_t)b * p.H_kv + hk) * stride;
+  const bool whole = (reinterpret_cast<uintptr_t>(sum) & 15) == 0;   // the interface asks for no more than floats
+#pragma unroll 1
   for (int j = (int)blockIdx.x * W_KEYS + (int)threadIdx.x * 4; j < L; j += (int)gridDim.x * W_KEYS) {
-    float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int g = 0; g < G; ++g) {
-      const float2 ml = p.final_ml[head0 + g];
-      const float4 x = *reinterpret_cast<const float4 *>(p.logits + (head0 + g) * slots + j);
-      const float c = -__fmul_rn(ml.x, lam), inv = ml.y > 0.0f ? __frcp_rn(ml.y) : 0.0f;
-      w[0] = __fmaf_rn(ex2_approx(__fmaf_rn(x.x, lam, c)), inv, w[0]);
-      w[1] = __fmaf_rn(ex2_approx(__fmaf_rn(x.y, lam, c)), inv, w[1]);
-      w[2] = __fmaf_rn(ex2_approx(__fmaf_rn(x.z, lam, c)), inv, w[2]);
-      w[3] = __fmaf_rn(ex2_approx(__fmaf_rn(x.w, lam, c)), inv, w[3]);
+    float4 x[G], w = make_float4(0.0f, 0.0f, 0.0f, 0.0f), old = w;
+#pragma unroll
+    for (int g = 0; g < G; ++g) x[g] = *reinterpret_cast<const float4 *>(p.logits + (head0 + g) * slots + j);
+    const bool four = whole && j + 3 < L;
+    if (four) {
+      old = *reinterpret_cast<const float4 *>(sum + j);
+    } else {
+      old.x = sum[j];
+      if (j + 1 < L) old.y = sum[j + 1];
+      if (j + 2 < L) old.z = sum[j + 2];
+      if (j + 3 < L) old.w = sum[j + 3];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (j + i < L) sum[j + i] = __fadd_rn(sum[j + i], w[i]);
+    for (int g = 0; g < G; ++g) {
+      const float c = -__fmul_rn(ml[g].x, lam), inv = ml[g].y > 0.0f ? __frcp_rn(ml[g].y) : 0.0f;
+      w.x = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].x, lam, c)), inv, w.x);
+      w.y = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].y, lam, c)), inv, w.y);
+      w.z = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].z, lam, c)), inv, w.z);
+      w.w = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].w, lam, c)), inv, w.w);
+    }
+    w.x = __fadd_rn(old.x, w.x), w.y = __fadd_rn(old.y, w.y), w.z = __fadd_rn(old.z, w.z), w.w = __fadd_rn(old.w, w.w);
+    if (four) {
+      *reinterpret_cast<float4 *>(sum + j) = w;
+    } else {
+      sum[j] = w.x;
+      if (j + 1 < L) sum[j + 1] = w.y;
+      if (j + 2 < L) sum[j + 2] = w.z;
+      if (j + 3 < L) sum[j + 3] = w.w;
+    }
   }
 }
 
@@ -1298,7 +1321,18 @@ extern "C" mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *q, const mpfa_
   if (rc != MPFA_OK) return rc;
   // a block for each chunk of keys where that is a few waves of blocks or less
   const int chunks = (slots + W_KEYS - 1) / W_KEYS, some = (16 * n_sm - 1) / (p.B * p.H_kv) + 1;
-  MPFA_CUDA_OK(launch(decode_weights_kernel, dim3((unsigned)(chunks < some ? chunks : some), (unsigned)p.H_kv, (unsigned)p.B), dim3(W_KEYS / 4), 0, s,
-                      p, weights, (size_t)weights_stride));
+  const dim3 grid((unsigned)(chunks < some ? chunks : some), (unsigned)p.H_kv, (unsigned)p.B);
+  void (*sums)(const DecodeParams, float *, size_t) = nullptr;
+  switch (p.H_q / p.H_kv) {
+    case 1: sums = decode_weights_kernel<1>; break;
+    case 2: sums = decode_weights_kernel<2>; break;
+    case 3: sums = decode_weights_kernel<3>; break;
+    case 4: sums = decode_weights_kernel<4>; break;
+    case 5: sums = decode_weights_kernel<5>; break;
+    case 6: sums = decode_weights_kernel<6>; break;
+    case 7: sums = decode_weights_kernel<7>; break;
+    default: sums = decode_weights_kernel<8>; break;
+  }
+  MPFA_CUDA_OK(launch(sums, grid, dim3(W_THREADS), 0, s, p, weights, (size_t)weights_stride));
   return MPFA_OK;
 }
