@@ -344,7 +344,7 @@ mpfa_status mpfa_decode(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, c
  * tile that visits its block (mpfa_quantize_v writes one for a NaN in its input only).
  * Here a seq_lens[b] above 64 * max_pages_per_req is treated as that bound in decode too.
  * Partitions of mpfa_decode_window are 1024 keys of the blocks that are not left out, so its workspace follows the window:
- * mpfa_decode_window_workspace_bytes().  max_pages_per_req of this section's calls is at most 2^24. */
+ * mpfa_decode_window_workspace_bytes().  max_pages_per_req (and new_max_pages) of this section's calls is at most 2^24, a seq_lens[b] below 0 counts as 0. */
 mpfa_status mpfa_prefill_window(const mpfa_fp4_tensor *h_q, const mpfa_fp4_tensor *h_k, const uint8_t *v_fp8,
                                 const void *delta_s_bf16, const mpfa_stats *h_stats, float v_scale, int window, int sinks,
                                 float softmax_scale, void *out_bf16, float *out_f32, int32_t *device_status, void *stream);
@@ -379,7 +379,7 @@ mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv 
  *   new_lens [B]          min(L, keep).
  *   new_weights [B, H_kv, new_weights_stride]  the kept tokens' weights, zeros after them (where new tokens' sums start).
  * weights_stride >= 64 * max_pages_per_req, new_weights_stride >= keep, sinks + recent <= keep, and new_weights and new_lens overlap weights
- * and seq_lens nowhere (else MPFA_ERR_INVALID_ARG).  seq_lens[b] above 64 * max_pages_per_req is treated as that bound, below 0 as 0.
+ * and seq_lens nowhere (else MPFA_ERR_INVALID_ARG).  seq_lens[b] above 64 * max_pages_per_req is treated as that bound.
  * A page-table entry outside [0, num_pages) raises MPFA_DEV_BAD_PAGE: tokens of such a source page become zeros, a page of new_table is left
  * out.  Decode works on the new pages as on any; since the kv heads keep different tokens, a slot no longer is a position. */
 mpfa_status mpfa_evict_paged(const mpfa_paged_kv *h_kv, const int32_t *page_table, int B, int max_pages_per_req,

@@ -215,7 +215,7 @@ struct DecodeParams {
   template <int MODE>
   __device__ __forceinline__ int length(int b) const {
     const int L = seq_lens[b];
-    return MODE == ALL_KEYS ? L : min(L, max_pages * PAGE);
+    return MODE == ALL_KEYS ? L : min(max(L, 0), max_pages * PAGE);
   }
   template <int MODE>
   __device__ __forceinline__ Span span(int L) const {

@@ -45,29 +45,16 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum over the block in thread order.  tmp: SEL_WARPS words, not written again before the block's next barrier.
-__device__ __forceinline__ uint32_t warp_scan(uint32_t x) {
-  const int lane = threadIdx.x & 31;
-  uint32_t s = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += a;
-  }
-  return s - x;
-}
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *tmp) {
+// What the warps before this one have, of a count for each warp in tmp.
+__device__ __forceinline__ uint32_t before_warp(const uint32_t *tmp) {
   static_assert(SEL_WARPS == 32, "a lane for each warp");
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t mine = warp_scan(x);
-  if (lane == 31) tmp[warp] = mine + x;
-  __syncthreads();
-  return mine + __shfl_sync(0xffffffffu, warp_scan(tmp[lane]), warp);   // every warp adds up the warps before it
+  const int lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, lane < (int)(threadIdx.x >> 5) ? tmp[lane] : 0u);
 }
 
 struct SelectShared {
   union {
-    uint32_t hist[BINS];
+    __align__(16) uint32_t hist[BINS];
     uint64_t list[LIST];
   };
   uint32_t tmp[2][SEL_WARPS], bin, need, inside, listed;
@@ -91,7 +78,7 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const float 
       const int bits = min(DIGIT, shift);
       shift -= bits;
       __syncthreads();   // of the pass before: bin, need, inside and the histogram have been read
-      for (int i = t; i < BINS; i += SEL_THREADS) sh.hist[i] = 0;
+      reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
       __syncthreads();
 #pragma unroll 4
       for (int i = first + t; i < last; i += SEL_THREADS) {
@@ -99,17 +86,26 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const float 
         if ((k & mask) == value) atomicAdd(&sh.hist[(uint32_t)(k >> shift) & ((1u << bits) - 1u)], 1u);
       }
       __syncthreads();
-      // a run of bins to a thread, the highest first: the bin in which the count from above reaches `need`
-      constexpr int PER = BINS / SEL_THREADS;
-      const int top = BINS - 1 - PER * t;
-      uint32_t c[PER], sum = 0;
+      // four bins to a lane, the highest first: the warp, then the lane and the bin in which the count from above reaches `need`
+      static_assert(BINS == 4 * SEL_THREADS, "four bins to a thread");
+      const uint4 c4 = reinterpret_cast<const uint4 *>(sh.hist)[SEL_THREADS - 1 - t];
+      const uint32_t c[4] = {c4.w, c4.z, c4.y, c4.x}, sum = (c[0] + c[1]) + (c[2] + c[3]), total = __reduce_add_sync(0xffffffffu, sum);
+      if (lane == 0) sh.tmp[0][warp] = total;
+      __syncthreads();
+      uint32_t above = before_warp(sh.tmp[0]);
+      if (above < need && need <= above + total) {
+        uint32_t incl = sum;
 #pragma unroll
-      for (int u = 0; u < PER; ++u) c[u] = sh.hist[top - u], sum += c[u];
-      uint32_t above = block_scan(sum, sh.tmp[0]);
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += v;
+        }
+        above += incl - sum;
 #pragma unroll
-      for (int u = 0; u < PER; ++u) {
-        if (above < need && need <= above + c[u]) sh.bin = (uint32_t)(top - u), sh.need = need - above, sh.inside = c[u];
-        above += c[u];
+        for (int u = 0; u < 4; ++u) {
+          if (above < need && need <= above + c[u]) sh.bin = (uint32_t)(BINS - 1 - 4 * t - u), sh.need = need - above, sh.inside = c[u];
+          above += c[u];
+        }
       }
       __syncthreads();
       value |= (uint64_t)sh.bin << shift;
@@ -142,8 +138,10 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const float 
   auto stays = [&](int i) { return i < end && (i < first || i >= last || key_of(w[i], i) >= border); };
   uint32_t count = 0;
 #pragma unroll 4
-  for (int i0 = begin; i0 < end; i0 += 32) count += stays(i0 + lane) ? 1u : 0u;
-  uint32_t to = __shfl_sync(0xffffffffu, block_scan(count, sh.tmp[1]), 0);
+  for (int i0 = begin; i0 < end; i0 += 32) count += __popc(__ballot_sync(0xffffffffu, stays(i0 + lane)));
+  if (lane == 0) sh.tmp[1][warp] = count;
+  __syncthreads();
+  uint32_t to = before_warp(sh.tmp[1]);
 #pragma unroll 4
   for (int i0 = begin; i0 < end; i0 += 32) {
     const bool s = stays(i0 + lane);
@@ -288,7 +286,7 @@ extern "C" mpfa_status mpfa_evict_paged(const mpfa_paged_kv *kv, const int32_t *
   if (B <= 0 || max_pages_per_req <= 0 || new_max_pages <= 0 || keep <= 0 || sinks < 0 || recent < 0) return MPFA_ERR_INVALID_ARG;
   if ((int64_t)sinks + recent > keep || (int64_t)new_max_pages * PAGE < keep) return MPFA_ERR_INVALID_ARG;
   if (kv->page_size != PAGE || kv->H_q % kv->H_kv != 0 || kv->H_q / kv->H_kv > 8) return MPFA_ERR_UNSUPPORTED;
-  if (max_pages_per_req > (1 << 24) || B > 65535 || kv->H_kv > 65535) return MPFA_ERR_UNSUPPORTED;
+  if (max_pages_per_req > (1 << 24) || new_max_pages > (1 << 24) || B > 65535 || kv->H_kv > 65535) return MPFA_ERR_UNSUPPORTED;
   if (weights_stride < max_pages_per_req * PAGE || new_weights_stride < keep) return MPFA_ERR_INVALID_ARG;
   const size_t heads = (size_t)B * kv->H_kv;
   if (overlap(weights, heads * weights_stride * sizeof(float), new_weights, heads * new_weights_stride * sizeof(float)) ||

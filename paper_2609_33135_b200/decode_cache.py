@@ -56,7 +56,36 @@ def build_cache(w: DecodeWorkload, device="cuda", smooth: bool = True, v_scale: 
                        torch.zeros(1, dtype=torch.int32, device=device), v_scale, w.softmax_scale)
 
 
-def decode_step(s: DecodeState) -> torch.Tensor:
-    B_.mpfa_decode(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, s.softmax_scale, s.out, s.out_f32,
-                   s.workspace, s.status)
+def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, weights: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One decode step.  window: the query sees the last `window` keys and the first `sinks` only.  weights [B, H_kv, >= 64 * pages]
+    (float32): what each key receives of the attention is added to it; of the whole context, so not together with a window."""
+    assert window is None or weights is None
+    if window is not None:
+        B_.mpfa_decode_window(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, window, sinks, s.softmax_scale, s.out, s.out_f32,
+                              s.workspace, s.status)
+    elif weights is not None:
+        B_.mpfa_decode_weights(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, s.softmax_scale, weights, s.out, s.out_f32,
+                               s.workspace, s.status)
+    else:
+        B_.mpfa_decode(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, s.softmax_scale, s.out, s.out_f32,
+                       s.workspace, s.status)
     return s.out
+
+
+def attention_sums(s: DecodeState) -> torch.Tensor:
+    """Zeroed sums for decode_step(weights=...), and a workspace of `s` that is large enough for it."""
+    s.workspace = B_.decode_weights_workspace(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1], s.page_table.device)
+    return torch.zeros(s.w.B, s.w.H_kv, s.page_table.shape[1] * B_.PAGE, device=s.page_table.device)
+
+
+def evict(s: DecodeState, weights: torch.Tensor, keep: int, sinks: int, recent: int, new_pages: torch.Tensor):
+    """Cuts every request's cache back to `keep` tokens a kv head, by `weights`, into the pages of new_pages [B, >= ceil(keep / 64)] (int32; of
+    the same pools, in no request's table); from then on `s` has those pages and lengths, and the old pages are the caller's again.
+    Returns (the kept tokens' former slots, their sums for further steps: a row is as wide as the new table)."""
+    dev = s.page_table.device
+    kept = torch.empty(s.w.B, s.w.H_kv, keep, dtype=torch.int32, device=dev)
+    new_lens = torch.empty_like(s.seq_lens)
+    new_weights = torch.empty(s.w.B, s.w.H_kv, new_pages.shape[1] * B_.PAGE, device=dev)
+    B_.mpfa_evict_paged(s.kv, s.page_table, s.seq_lens, weights, keep, sinks, recent, new_pages, kept, new_lens, new_weights, s.status)
+    s.page_table, s.seq_lens = new_pages, new_lens
+    return kept, new_weights

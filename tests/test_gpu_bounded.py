@@ -621,3 +621,109 @@ def test_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for want, (_, out, status) in zip(alone, bufs):
         assert int(status) == 0 and torch.equal(out, want)
+
+
+def test_the_cache_module_serves_bounded_requests():
+    """decode_cache's own calls: a window, sums of the weights, and eviction after which the request goes on with its new pages."""
+    from paper_2609_33135_b200 import decode_cache
+    B = binding()
+    st = state(1220, [900, 300], 8, 2)
+    want, _ = window_decode(st, 200, 5)
+    assert torch.equal(decode_cache.decode_step(st, window=200, sinks=5), want)
+    sums = decode_cache.attention_sums(st)
+    decode_cache.decode_step(st, weights=sums)
+    pages, n, big = 5, st.kv.num_pages, B.PagedKV.empty(st.kv.num_pages + 10, 8, 2)
+    for new, old in ((big.k_codes, st.kv.k_codes), (big.k_sf, st.kv.k_sf), (big.v_fp8, st.kv.v_fp8), (big.delta, st.kv.delta)):
+        new[:n] = old
+    st.kv = big
+    new_pages = torch.arange(n, n + 10, dtype=torch.int32, device="cuda").view(2, pages)
+    kept, new_sums = decode_cache.evict(st, sums, 300, 4, 100, new_pages)
+    assert st.seq_lens.tolist() == [300, 300] and new_sums.shape == (2, 2, 320)
+    for hk in range(2):
+        assert kept[0, hk].tolist() == plain.evicted(sums[0, hk].cpu().numpy(), 900, 300, 4, 100).tolist()
+        assert kept[1, hk].tolist() == list(range(300))
+    before = new_sums.clone()
+    decode_cache.decode_step(st, weights=new_sums)
+    torch.cuda.synchronize()
+    assert int(st.status) == 0
+    assert torch.allclose((new_sums - before).sum(2), torch.full((2, 2), 4.0, device="cuda"), rtol=2.0 ** -12)
+
+
+def test_lengths_below_zero_count_as_none():
+    B = binding()
+    st = state(1230, [300, 200, 100], 4, 2)
+    want, _ = window_decode(st, 50, 2)
+    st.seq_lens[1] = -(2 ** 31)
+    out, o32 = window_decode(st, 50, 2)
+    assert torch.equal(out[0::2], want[0::2]) and not o32[1].any()
+    weights = torch.zeros(3, 2, st.page_table.shape[1] * 64, device="cuda")
+    out, o32 = weights_decode(st, weights)
+    assert not o32[1].any() and not weights[1].any() and bool(weights[0, :, :300].all())
+    q4 = B.Fp4Tensor.empty(3, 4, 9)
+    B.mpfa_quantize_qk(torch.randn(3, 9, 4, 128, device="cuda").bfloat16(), None, B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    o = torch.full((3, 9, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mpfa_prefill_paged_window(q4, st.kv, st.page_table, st.seq_lens, st.stats, 1.0, 50, 2, st.softmax_scale, o, None, status)
+    assert int(status) == 0 and not o[1].any() and bool(o[0].any())
+    kv, table, spare = pool(1231, [300, 200], 4, 2, 4)
+    lens = torch.tensor([-5, 200], dtype=torch.int32, device="cuda")
+    w = torch.rand(2, 2, table.shape[1] * 64).cuda()
+    kept, new_lens, new_weights, status = evict(kv, table, lens, w, 100, 4, 4, spare.view(2, 2))
+    assert status == 0 and new_lens.tolist() == [0, 100] and (kept[0] == -1).all() and not new_weights[0].any()
+
+
+def test_nothing_is_written_outside_the_buffers():
+    """Every buffer that these calls write, workspaces of exactly the size that is asked for among them, cut out of one arena with guard bands
+    whose bytes have to stay."""
+    B = binding()
+    arena, cuts, at = torch.full((64 << 20,), 0xA5, dtype=torch.uint8, device="cuda"), [], [0]
+
+    def cut(n, dtype=torch.uint8, shape=None):
+        begin = (at[0] + 4096 + 1023) // 1024 * 1024
+        at[0] = begin + n
+        cuts.append((begin, begin + n))
+        t = arena[begin:begin + n].view(dtype)
+        return t if shape is None else t.view(shape)
+
+    def intact():
+        torch.cuda.synchronize()
+        last = 0
+        for a, b in cuts + [(arena.numel(), arena.numel())]:
+            assert bool((arena[last:a] == 0xA5).all()), (last, a)
+            last = b
+
+    st = state(1240, [2500, 1, 130], 10, 2)
+    P, n = st.page_table.shape[1], st.kv.num_pages
+    status = cut(4, torch.int32)
+    status.zero_()
+    out, o32 = cut(3 * 10 * 256, torch.bfloat16, (3, 10, 128)), cut(3 * 10 * 512, torch.float32, (3, 10, 128))
+    L = B.lib()
+    ws = cut(L.mpfa_decode_window_workspace_bytes(3, 10, 2, P, 1100, 200))
+    B.mpfa_decode_window(st.q4, st.kv, st.page_table, st.seq_lens, st.stats, 1.0, 1100, 200, st.softmax_scale, out, o32, ws, status)
+    intact()
+    ws = cut(L.mpfa_decode_weights_workspace_bytes(3, 10, 2, P))
+    weights = cut(3 * 2 * P * 64 * 4, torch.float32, (3, 2, P * 64))
+    weights.zero_()
+    B.mpfa_decode_weights(st.q4, st.kv, st.page_table, st.seq_lens, st.stats, 1.0, st.softmax_scale, weights, out, o32, ws, status)
+    intact()
+    keep, per = 333, 6
+    kv = B.PagedKV(cut((n + 3 * per) * 2 * 4096, shape=(-1, 2, 4096)), cut((n + 3 * per) * 2 * 512, shape=(-1, 2, 512)),
+                   cut((n + 3 * per) * 2 * 8192, shape=(-1, 2, 8192)), cut((n + 3 * per) * 10 * 128, torch.bfloat16, (-1, 10, 64)), n + 3 * per, 10, 2)
+    for new, old in ((kv.k_codes, st.kv.k_codes), (kv.k_sf, st.kv.k_sf), (kv.v_fp8, st.kv.v_fp8), (kv.delta, st.kv.delta)):
+        new[:n] = old
+    new_table = torch.arange(n, n + 3 * per, dtype=torch.int32, device="cuda").view(3, per)
+    kept, new_lens = cut(3 * 2 * keep * 4, torch.int32, (3, 2, keep)), cut(12, torch.int32)
+    new_weights = cut(3 * 2 * 335 * 4, torch.float32, (3, 2, 335))
+    B.mpfa_evict_paged(kv, st.page_table, st.seq_lens, weights, keep, 4, 50, new_table, kept, new_lens, new_weights, status)
+    intact()
+    q4 = B.Fp4Tensor.empty(3, 10, 131)
+    B.mpfa_quantize_qk(torch.randn(3, 131, 10, 128, device="cuda").bfloat16(), None, B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    rows, r32 = cut(3 * 131 * 10 * 256, torch.bfloat16, (3, 131, 10, 128)), cut(3 * 131 * 10 * 512, torch.float32, (3, 131, 10, 128))
+    B.mpfa_prefill_paged_window(q4, kv, new_table, new_lens, st.stats, 1.0, 70, 9, st.softmax_scale, rows, r32, status)
+    intact()
+    w = wl.prefill_workload("guards", 1241, 1, 300, 10, 2, True)
+    s1 = B.stage1(w.q.cuda(), w.k.cuda(), w.v.cuda())
+    B.mpfa_prefill_window(s1.q, s1.k, s1.v_fp8, s1.delta, s1.stats, 1.0, 70, 9, w.softmax_scale, cut(300 * 2560, torch.bfloat16),
+                          cut(300 * 5120, torch.float32), status)
+    intact()
+    assert int(status) == 0 and new_lens.tolist() == [333, 1, 130] and at[0] < arena.numel()
