@@ -56,9 +56,8 @@
 // (mpfa_decode_window); every key, with the logits kept so that what each key received can be added to its running sum
 // (mpfa_decode_weights).
 //
-// Window.  Visible are the keys j >= low = L - window and j < sinks.  The blocks that hold one are numbered as if the blocks between the
-// two ranges did not exist (struct Span), and partitions, tickets and states count in those numbers; only addresses and masks use the
-// token's own index.  A page without a visible key is neither looked at nor copied, so its table entry may be stale, and of the V rows
+// Window.  Visible are the keys j >= L - window and j < sinks.  Keys are counted as if the 128-key blocks between the two ranges did not
+// exist (struct Span); only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor copied, so its table entry may be stale, and of the V rows
 // of a page that is visible in part the others are zeros: a hidden token's V may be anything, NaN included, and 0 x NaN is not 0.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -184,11 +183,11 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
-// The keys of a request as its work items count them.  Blocks [0, heads) are the sinks', then `shift` blocks are left out.
+// The keys of a request as its work items count them: blocks [0, heads) are the sinks', then `shift` blocks are left out.
 struct Span {
-  int low;          // first key of the window
-  int heads, shift; // 0, 0 where nothing is left out
-  int len;          // keys, without those of the blocks that are left out
+  int len;          // keys
+  int low;          // first key of the window; not below 128 heads, nor is `sinks` above that, where blocks are left out
+  int heads, shift; // 0, 0 where none are
 };
 
 struct DecodeParams {
@@ -219,19 +218,17 @@ struct DecodeParams {
   }
   template <int MODE>
   __device__ __forceinline__ Span span(int L) const {
-    if constexpr (MODE != WINDOW) return Span{0, 0, 0, L};
-    const int low = max(L - window, 0), heads = (min(sinks, low) + TILE - 1) / TILE, gap = low / TILE - heads;
-    return gap > 0 ? Span{low, heads, gap, L - gap * TILE} : Span{low, 0, 0, L};
+    if constexpr (MODE != WINDOW) return Span{L, 0, 0, 0};
+    const int low = max(L - window, 0), heads = (min(sinks, low) + TILE - 1) / TILE, gap = max(low / TILE - heads, 0);
+    return Span{L - gap * TILE, low - gap * TILE, gap > 0 ? heads : 0, gap};
   }
   template <int MODE>
   __device__ __forceinline__ int n_parts(int L) const {
     return min((max(span<MODE>(L).len, 0) + DECODE_SPLIT - 1) / DECODE_SPLIT, n_split);
   }
-  // first token of a block
-  static __device__ __forceinline__ int block_key(const Span &sp, int block) { return (block + (block >= sp.heads ? sp.shift : 0)) * TILE; }
   template <int MODE>
-  __device__ __forceinline__ bool visible(const Span &sp, int key, int L) const {
-    return key < L && (MODE != WINDOW || key >= sp.low || key < sinks);
+  __device__ __forceinline__ bool visible(const Span &sp, int key) const {
+    return key < sp.len && (MODE != WINDOW || key >= sp.low || key < sinks);
   }
 };
 
@@ -311,7 +308,7 @@ struct WorkIter {
 __device__ __forceinline__ void lookup_pages(const DecodeParams &p, const WorkIter &w, int lane, int &pid0, int &pid1) {
   pid0 = -1, pid1 = -1;
   if (lane < w.nblk) {
-    const int pg = DecodeParams::block_key(w.span, w.sp * MAXBLK + lane) / PAGE;
+    const int block = w.sp * MAXBLK + lane, pg = (block + (block >= w.span.heads ? w.span.shift : 0)) * (TILE / PAGE);
     const int32_t *row = p.page_table + (size_t)w.b * p.max_pages;
     if (pg < p.max_pages) pid0 = row[pg];
     if (pg + 1 < p.max_pages) pid1 = row[pg + 1];
@@ -531,9 +528,9 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       // Nothing can be done with V before the first item's softmax, and while all CTAs start at once its copies only keep K waiting, of
       // which warp 17's last block may still be to come.
       if (!is_k && j == 0) ok = cx.wait_warp(B_V_GO, 0);
-      const int key0 = DecodeParams::block_key(w.span, w.sp * MAXBLK + lane);
+      const int key0 = w.sp * DECODE_SPLIT + lane * TILE;
       const bool in = lane < w.nblk;
-      bool want0 = true, want1 = key0 + PAGE < w.L;
+      bool want0 = true, want1 = key0 + PAGE < w.span.len;
       // rows of the two pages between the sinks' end and the window's beginning: of a page that is all of it nothing is wanted, of another
       // one V takes these as zeros
       int hide0 = 0, show0 = 0, hide1 = 0, show1 = 0;
@@ -765,6 +762,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       float *xm = xmax + par * MAXBLK * MAXG * 4, *wt = wtab + par * MAXBLK * MAXG, *xlg = xl + par * 8 * MAXG;
       const float lam = w.b < D_MAXREQ ? lam_tab[w.b]
                                        : __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[w.b]), p.k_gscale[w.b]);
+      const int k_part = w.sp * DECODE_SPLIT;
       // ---- all scores of the item at once.  They are read from tensor memory twice, once for the maxima and once for the
       // exponentials: held in registers in between, MAXBLK x G of them and as many maxima went to local memory for groups
       // of five heads and more (24 us per item instead of 6).
@@ -783,7 +781,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         for (int u = 0; u < CH; ++u) {
           const int t = t0 + 2 * u;
           if (t < w.nblk) {
-            const bool valid = p.visible<MODE>(w.span, DecodeParams::block_key(w.span, w.sp * MAXBLK + w.nblk - 1 - t) + r, w.L);
+            const bool valid = p.visible<MODE>(w.span, k_part + (w.nblk - 1 - t) * TILE + r);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               const float wm = warp_max(valid ? __uint_as_float(sr[u][g]) : -INFINITY);
@@ -837,12 +835,12 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
           for (int u = 0; u < CH; ++u) {
             const int t = v * TPV + t0 + 2 * u;
             if (t < w.nblk) {
-              const bool valid = p.visible<MODE>(w.span, DecodeParams::block_key(w.span, w.sp * MAXBLK + w.nblk - 1 - t) + r, w.L);
+              const bool valid = p.visible<MODE>(w.span, k_part + (w.nblk - 1 - t) * TILE + r);
               float pq[G + 1];
               if constexpr (MODE == WEIGHTS) {
                 if (valid) {
                   const size_t slots = (size_t)p.max_pages * PAGE;
-                  float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + (w.sp * MAXBLK + w.nblk - 1 - t) * TILE + r;
+                  float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + k_part + (w.nblk - 1 - t) * TILE + r;
 #pragma unroll
                   for (int g = 0; g < G; ++g) x[g * slots] = __uint_as_float(sr[u][g]);
                 }

@@ -35,9 +35,9 @@ struct EvictParams {
 
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
 constexpr int DIGIT = 12, BINS = 1 << DIGIT;
-constexpr int LIST = 256;          // ranking m candidates against one another takes about m^2 / 32 cycles, a digit 2500
+constexpr int LIST = SEL_THREADS / 4;   // ranked against one another by four threads each
 constexpr int SEL_CACHE = 49152;   // weights held in shared memory between the passes: 192 KB
-constexpr int SEL_AHEAD = 8;       // loads of a thread on the way
+constexpr int SEL_AHEAD = 4;       // loads of a thread on the way
 
 __device__ __forceinline__ uint32_t order_of(float w) {
   if (w != w) return 0u;
@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t before_warp(const uint32_t *tmp) {
 }
 
 struct SelectShared {
-  union {
+  union {   // the list is made when the last histogram has been read
     __align__(16) uint32_t hist[BINS];
     uint64_t list[LIST];
   };
@@ -61,29 +61,36 @@ struct SelectShared {
   uint64_t border;
 };
 
-__device__ __forceinline__ uint64_t key_of(float w, int slot) { return (uint64_t)order_of(w) << 32 | (0xffffffffu - (uint32_t)slot); }
-
-// The slots kept of n > keep, to kept[] in ascending order.  w: shared or global memory.
-template <bool SHARED>
-__device__ __forceinline__ void select_tokens(const EvictParams &p, const float *w, int n, int32_t *kept, SelectShared &sh) {
+// The slots kept of n > keep, to kept[] in ascending order.  HELD: `held` has the orders of all weights, and sh.hist the counts of the
+// candidates' first digits; otherwise both are made from the weights w in global memory.
+template <bool HELD>
+__device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32_t *held, const float *w, int n, int32_t *kept, SelectShared &sh) {
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const int first = p.sinks, last = n - p.recent;   // the candidates: [first, last)
+  auto order = [&](int i) { return HELD ? held[i] : order_of(w[i]); };
   uint32_t need = (uint32_t)(p.keep - p.sinks - p.recent);
-  uint64_t border = ~0ull;   // no key is as large
+  uint32_t least = 0xffffffffu;   // no weight has this order
+  int slot = -1;                  // of those of the least order, the last that stays
   if (need > 0) {
-    uint64_t value = 0, mask = 0;
-    int shift = 64;
+    // the digits so far, of the orders and then of the slots' complements
+    uint32_t value = 0, mask = 0, s_value = 0, s_mask = 0;
+    int shift = 32;
+    bool by_slot = false, counted = HELD;
 #pragma unroll 1
-    for (uint32_t inside = (uint32_t)(last - first); inside > LIST;) {
+    for (uint32_t inside = (uint32_t)(last - first); inside > LIST; counted = false) {
+      if (shift == 0) shift = 32, by_slot = true;
       const int bits = min(DIGIT, shift);
       shift -= bits;
-      __syncthreads();   // of the pass before: bin, need, inside and the histogram have been read
-      reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
-      __syncthreads();
-#pragma unroll 4
-      for (int i = first + t; i < last; i += SEL_THREADS) {
-        const uint64_t k = key_of(w[i], i);
-        if ((k & mask) == value) atomicAdd(&sh.hist[(uint32_t)(k >> shift) & ((1u << bits) - 1u)], 1u);
+      const uint32_t digit = (1u << bits) - 1u;
+      if (!counted) {
+        __syncthreads();   // of the pass before: bin, need, inside and the histogram have been read
+        reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+#pragma unroll 2
+        for (int i = first + t; i < last; i += SEL_THREADS) {
+          const uint32_t u = order(i), s = ~(uint32_t)i;
+          if ((u & mask) == value && (s & s_mask) == s_value) atomicAdd(&sh.hist[((by_slot ? s : u) >> shift) & digit], 1u);
+        }
       }
       __syncthreads();
       // four bins to a lane, the highest first: the warp, then the lane and the bin in which the count from above reaches `need`
@@ -107,52 +114,65 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const float 
           above += c[u];
         }
       }
+      if (t == 0) sh.listed = 0;
       __syncthreads();
-      value |= (uint64_t)sh.bin << shift;
-      mask |= (uint64_t)((1u << bits) - 1u) << shift;
+      (by_slot ? s_value : value) |= sh.bin << shift;
+      (by_slot ? s_mask : mask) |= digit << shift;
       need = sh.need, inside = sh.inside;
     }
-    // the candidates of that bin, in any order; the one with need - 1 larger ones is the border
+    // the candidates of that bin, in any order; the one with need - 1 larger ones is the last that stays
     __syncthreads();
-    if (t == 0) sh.listed = 0;
-    __syncthreads();
+    if (mask == 0) {   // no digit was needed
+      if (t == 0) sh.listed = 0;
+      __syncthreads();
+    }
 #pragma unroll 4
     for (int i = first + t; i < last; i += SEL_THREADS) {
-      const uint64_t k = key_of(w[i], i);
-      if ((k & mask) == value) sh.list[atomicAdd(&sh.listed, 1u)] = k;
+      const uint32_t u = order(i), s = ~(uint32_t)i;
+      if ((u & mask) == value && (s & s_mask) == s_value) sh.list[atomicAdd(&sh.listed, 1u)] = (uint64_t)u << 32 | s;
     }
     __syncthreads();
+    // four threads to a candidate
     const int m = (int)sh.listed;
-    if (t < m) {
-      const uint64_t mine = sh.list[t];
+    if (warp * 8 < m) {
+      const uint64_t mine = (t >> 2) < m ? sh.list[t >> 2] : ~0ull;
       uint32_t larger = 0;
-#pragma unroll 8
-      for (int i = 0; i < m; ++i) larger += sh.list[i] > mine ? 1u : 0u;
-      if (larger == need - 1) sh.border = mine;
+#pragma unroll 4
+      for (int i = t & 3; i < m; i += 4) larger += sh.list[i] > mine ? 1u : 0u;
+      larger += __shfl_xor_sync(0xffffffffu, larger, 1);
+      larger += __shfl_xor_sync(0xffffffffu, larger, 2);
+      if ((t >> 2) < m && larger == need - 1) sh.border = mine;
     }
     __syncthreads();
-    border = sh.border;
+    least = (uint32_t)(sh.border >> 32), slot = (int)~(uint32_t)sh.border;
   }
   // In the order of the slots: each warp takes a run of them, counts, and writes when it knows what the warps before it have.
   const int run = ((n + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, begin = min(warp * run, n), end = min(begin + run, n);
-  auto stays = [&](int i) { return i < end && (i < first || i >= last || key_of(w[i], i) >= border); };
-  uint32_t count = 0;
-#pragma unroll 4
-  for (int i0 = begin; i0 < end; i0 += 32) count += __popc(__ballot_sync(0xffffffffu, stays(i0 + lane)));
+  auto stays = [&](int i) {
+    if (i >= end) return false;
+    const uint32_t u = order(i);
+    return i < first || i >= last || u > least || (u == least && i <= slot);
+  };
+  uint32_t count = 0, answers = 0;   // of the first 32 groups of 32 slots lane k keeps the k-th answer
+#pragma unroll 2
+  for (int i0 = begin, k = 0; i0 < end; i0 += 32, ++k) {
+    const uint32_t bits = __ballot_sync(0xffffffffu, stays(i0 + lane));
+    count += __popc(bits);
+    if (k == lane) answers = bits;
+  }
   if (lane == 0) sh.tmp[1][warp] = count;
   __syncthreads();
   uint32_t to = before_warp(sh.tmp[1]);
-#pragma unroll 4
-  for (int i0 = begin; i0 < end; i0 += 32) {
-    const bool s = stays(i0 + lane);
-    const uint32_t bits = __ballot_sync(0xffffffffu, s);
-    if (s) kept[to + __popc(bits & ((1u << lane) - 1u))] = i0 + lane;
+#pragma unroll 2
+  for (int i0 = begin, k = 0; i0 < end; i0 += 32, ++k) {
+    const uint32_t bits = k < 32 ? __shfl_sync(0xffffffffu, answers, k) : __ballot_sync(0xffffffffu, stays(i0 + lane));
+    if (bits >> lane & 1u) kept[to + __popc(bits & ((1u << lane) - 1u))] = i0 + lane;
     to += __popc(bits);
   }
 }
 
 __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ float held[];             // the weights, where they fit
+  extern __shared__ uint32_t held[];          // the orders of the weights, where they fit
   __shared__ SelectShared sh;
   grid_dependency_wait();
   launch_dependents();
@@ -167,26 +187,34 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
 #pragma unroll
   for (int u = 0; u < SEL_AHEAD; ++u) x[u] = t + u * SEL_THREADS < most ? w[t + u * SEL_THREADS] : 0.0f;
   const int n = p.length(b), count = min(n, p.keep);
+  reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
   if (hk == 0 && t == 0) p.new_lens[b] = count;
   for (size_t i = (size_t)count + t; i < p.new_stride; i += SEL_THREADS) out[i] = 0.0f;
   for (int i = count + t; i < p.keep; i += SEL_THREADS) kept[i] = -1;
   if (n <= p.keep) {
     for (int i = t; i < n; i += SEL_THREADS) kept[i] = i;
   } else if (n <= SEL_CACHE) {
+    __syncthreads();
+#pragma unroll 1
+    for (int i0 = t;;) {
 #pragma unroll
-    for (int u = 0; u < SEL_AHEAD; ++u)
-      if (t + u * SEL_THREADS < n) held[t + u * SEL_THREADS] = x[u];
-    for (int i = t + SEL_AHEAD * SEL_THREADS; i < n; i += SEL_AHEAD * SEL_THREADS) {
+      for (int u = 0; u < SEL_AHEAD; ++u) {
+        const int i = i0 + u * SEL_THREADS;
+        if (i < n) {
+          const uint32_t o = order_of(x[u]);
+          held[i] = o;
+          if (i >= p.sinks && i < n - p.recent) atomicAdd(&sh.hist[o >> (32 - DIGIT)], 1u);
+        }
+      }
+      i0 += SEL_AHEAD * SEL_THREADS;
+      if (i0 >= n) break;
 #pragma unroll
-      for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i + u * SEL_THREADS < n ? w[i + u * SEL_THREADS] : 0.0f;
-#pragma unroll
-      for (int u = 0; u < SEL_AHEAD; ++u)
-        if (i + u * SEL_THREADS < n) held[i + u * SEL_THREADS] = x[u];
+      for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i0 + u * SEL_THREADS < n ? w[i0 + u * SEL_THREADS] : 0.0f;
     }
     __syncthreads();
-    select_tokens<true>(p, held, n, kept, sh);
+    select_tokens<true>(p, held, w, n, kept, sh);
   } else {
-    select_tokens<false>(p, w, n, kept, sh);
+    select_tokens<false>(p, held, w, n, kept, sh);
   }
 }
 
