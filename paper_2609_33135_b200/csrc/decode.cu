@@ -59,6 +59,16 @@
 // Window.  Visible are the keys j >= L - window and j < sinks.  Keys are counted as if the 128-key blocks between the two ranges did not
 // exist (struct Span); only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor copied, so its table entry may be stale, and of the V rows
 // of a page that is visible in part the others are zeros: a hidden token's V may be anything, NaN included, and 0 x NaN is not 0.
+// Whole calls back to back: one request under a window of 1024 13.9 us (three kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
+// of cache) 89 us, 4.7 TB/s; 32 under 16384 (0.88 GB) 150 us, 5.9 TB/s.  Windows rarely end with a partition, so one item in five of the
+// 64 requests has one or two blocks, and such an item costs 2 us whatever it holds (instruction fetch: 2.0 stalled warps per issue for
+// want of an instruction, 0.6 where all items are long).  Masks made from tokens' own indices, with the block looked up for every one: 91.4.
+//
+// Weights.  The logits stay in FP32: 4 G bytes per key written, and read back by decode_weights_kernel once the merge has the (m, l) of the
+// whole request; recomputing them instead would read K, its scales and Delta_S again (72 + 2 G).  One request of 4097 keys 15.6 us (mpfa_decode
+// alone 12.9), 64 of 1000..8192, 40:8 heads, 118 (97.5; 0.55 GB of cache, and 0.1 of logits written and read).  Not kept: merge and sums in
+// one kernel (126 and 15.4); an L2 policy that lets the logits outlive the cache's bytes (they then come from L2, 12.5 us for the sums
+// instead of 15.5 alone, but the whole is no shorter: 119); the next chunk on its way during a sum, with 4 to 16 blocks per SM (118 to 119).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
@@ -1081,7 +1091,8 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
 // What each key received: weights[b, kv head, j] += sum over the group's heads of 2^(lam (S_j - m)) / l, in FP32 from the logits that the
 // split kernel kept and the (m, l) of the whole request.  A thread takes four keys, a block chunks of 1024, heads in ascending order: one
 // writer per sum, a fixed order.  Bound by memory: 4 G bytes of logits per key read back, 8 of the sum; and at its beginning by three loads
-// that wait for one another (length, logits, and the merge's (m, l) beside them), which is why all heads' are asked for at once.
+// that wait for one another (length, logits, and the merge's (m, l) beside them), which is why all heads' are asked for at once (head after
+// head 17.3 us for 301000 keys x 8 kv heads of five, so 14.5: 4.6 TB/s).
 constexpr int W_KEYS = 1024, W_THREADS = W_KEYS / 4;
 template <int G>
 __global__ void __launch_bounds__(W_THREADS) decode_weights_kernel(const __grid_constant__ DecodeParams p, float *weights, size_t stride) {

@@ -212,7 +212,16 @@ __device__ __forceinline__ float exponent_unit(const PrefillParams &p, int b) {
 // result is explained beyond the compiler's schedules, which differ in every role: the rule is what was measured.
 //
 // WINDOW: a sliding window and sinks.  An item's list of blocks leaves out those between the sinks and the window of the tile's first
-// row; everything else is a matter of addresses and masks (struct Tile, hidden()).
+// row; everything else is a matter of addresses and masks (struct Tile, visible32()).  An item has up to five blocks with a mask (the window's
+// two ends lie in two blocks each, the sinks' last block) where the causal kernel has one or two, so masks are made as sets of 32 bits and
+// voted on per 32 keys: compared key by key, 4001 tokens under 1024 (32:8 heads) took 77 us, 16384 under 4096 821, chunks of 512 under 2048 on
+// pages 164; so 73, 766 and 98 (0.80, 1.27 and 0.70 PFLOP/s of visible pairs; a window as wide as the context costs what causal attention
+// costs, on pages 5 % more).  Contiguous operands take the first form of LONG at every length (16384 under 4096 766 / 806, 4001 under 1024 73 /
+// 78), pages the second (2048-key windows 111 / 96; windows of 512 keys 51 / 53).
+// What bounds it is what bounds the causal kernel, a chain of hand-overs per block and the accumulator's per item; of what is visited, one
+// block in eight for a window of 1024 lies half outside it, and four sinks cost a block.  Not kept, each slower everywhere because a role's
+// code costs the other roles their instruction cache: exponentials left out for 32 keys that no row sees (16384 under 4096 1184 us),
+// a path of its own for the sinks' block (831), rows sent out through shared memory so that the accumulator is free earlier (792 to 824).
 template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false>
 __global__ void __launch_bounds__(NTHREADS, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -506,7 +515,6 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           pin32(x);
           if constexpr (WINDOW) {
             if (ragged) {
-              // an item has up to five such blocks, at most two chunks of each mixed for a warp's rows: the others cost a vote
               const uint32_t see = visible32(key0 + c0, limit, low, p.sinks);
               if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
 #pragma unroll
