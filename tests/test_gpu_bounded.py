@@ -727,3 +727,60 @@ def test_nothing_is_written_outside_the_buffers():
                           cut(300 * 5120, torch.float32), status)
     intact()
     assert int(status) == 0 and new_lens.tolist() == [333, 1, 130] and at[0] < arena.numel()
+
+
+def test_without_compensation_on_pages():
+    """A cache without a Delta_S pool: decode with a window, decode with weights, a chunk under a window."""
+    B = binding()
+    st = state(1250, [1300, 77], 10, 2, v_scale=2.0, smooth=False)
+    assert st.kv.delta is None
+    out, o32 = window_decode(st, 333, 40)
+    rounded(out, o32)
+    check_window_decode(st, 333, 40, o32)
+    weights = torch.zeros(2, 2, st.page_table.shape[1] * 64, device="cuda")
+    weights_decode(st, weights)
+    for b, L in enumerate((1300, 77)):
+        want = plain_weights(st, b)
+        close(weights[b, :, :L].cpu().numpy(), want, (2 * plain.NEAR + 2.0 ** -24) * want, b)
+    q4 = B.Fp4Tensor.empty(2, 10, 60)
+    B.mpfa_quantize_qk(torch.randn(2, 60, 10, 128, generator=torch.Generator().manual_seed(3)).bfloat16().cuda(), None, B.MPFA_STATS_FROZEN,
+                       st.stats, q4, None, None, None)
+    o32, status = torch.empty(2, 60, 10, 128, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mpfa_prefill_paged_window(q4, st.kv, st.page_table, st.seq_lens, st.stats, 2.0, 200, 3, st.softmax_scale,
+                                torch.empty(2, 60, 10, 128, dtype=torch.bfloat16, device="cuda"), o32, status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    Q = plain.tile_rows(q4)
+    for b, L in enumerate((1300, 77)):
+        K, V, D = plain.cached(st.kv, st.page_table[b].cpu().numpy(), L)
+        check_rows(Q[b], K, V, D, o32[b].cpu().numpy(), np.arange(60) + L - 60, 200, 3, plain.lam_of(st.stats, b, st.softmax_scale), 2.0, (10, 2), b)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_windows_drawn(seed):
+    """Drawn lengths, windows, sinks and groups, decode and a chunk of the same requests."""
+    B, r = binding(), np.random.RandomState(seed)
+    H_q, H_kv = [(4, 2), (8, 1), (6, 2), (5, 1)][seed % 4]
+    lens = [int(x) for x in np.exp(r.uniform(0, np.log(2400), 3))]
+    window, sinks, N_q = int(np.exp(r.uniform(0, np.log(2500)))), int(r.choice([0, 1, 5, 64, 100, 129, 400])), int(r.randint(1, 300))
+    st = state(1300 + seed, lens, H_q, H_kv, v_scale=0.5)
+    out, o32 = window_decode(st, window, sinks)
+    rounded(out, o32)
+    check_window_decode(st, window, sinks, o32)
+    q_lens = [min(N_q, L) for L in lens]
+    q4 = B.Fp4Tensor.empty(3, H_q, N_q)
+    B.mpfa_quantize_qk(torch.randn(3, N_q, H_q, 128, generator=torch.Generator().manual_seed(seed)).bfloat16().cuda(), None,
+                       B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    o32, status = torch.empty(3, N_q, H_q, 128, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mpfa_prefill_paged_window(q4, st.kv, st.page_table, st.seq_lens, st.stats, 0.5, window, sinks, st.softmax_scale,
+                                torch.empty(3, N_q, H_q, 128, dtype=torch.bfloat16, device="cuda"), o32, status,
+                                torch.tensor(q_lens, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    Q = plain.tile_rows(q4)
+    for b, L in enumerate(lens):
+        K, V, D = plain.cached(st.kv, st.page_table[b].cpu().numpy(), L)
+        n = q_lens[b]
+        check_rows(Q[b, :, :n], K, V, D, o32[b, :n].cpu().numpy(), np.arange(n) + L - n, window, sinks, plain.lam_of(st.stats, b, st.softmax_scale),
+                   0.5, (H_q, H_kv), b)
+        assert not o32[b, n:].any()
