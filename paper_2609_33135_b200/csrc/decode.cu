@@ -57,9 +57,10 @@
 // (mpfa_decode_weights).
 //
 // Window.  Visible are the keys j >= L - window and j < sinks.  Keys are counted as if the 128-key blocks between the two ranges did not
-// exist (struct Span); only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor copied, so its table entry may be stale, and of the V rows
-// of a page that is visible in part the others are zeros: a hidden token's V may be anything, NaN included, and 0 x NaN is not 0.
-// Whole calls back to back: one request under a window of 1024 13.9 us (three kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
+// exist (struct Span); only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor
+// copied, so its table entry may be stale, and of the V rows of a page that is visible in part the others are zeros: a hidden token's V may
+// be anything, NaN included, and 0 x NaN is not 0.
+// Whole calls back to back: one request under a window of 1024 13.9 us (two kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
 // of cache) 89 us, 4.7 TB/s; 32 under 16384 (0.88 GB) 150 us, 5.9 TB/s.  Windows rarely end with a partition, so one item in five of the
 // 64 requests has one or two blocks, and such an item costs 2 us whatever it holds (instruction fetch: 2.0 stalled warps per issue for
 // want of an instruction, 0.6 where all items are long).  Masks made from tokens' own indices, with the block looked up for every one: 91.4.

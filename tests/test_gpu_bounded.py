@@ -784,3 +784,43 @@ def test_windows_drawn(seed):
         check_rows(Q[b, :, :n], K, V, D, o32[b, :n].cpu().numpy(), np.arange(n) + L - n, window, sinks, plain.lam_of(st.stats, b, st.softmax_scale),
                    0.5, (H_q, H_kv), b)
         assert not o32[b, n:].any()
+
+
+def test_pools_of_more_than_four_gigabytes():
+    """Slabs whose byte offsets do not fit 32 bits: the pages of a small cache moved to the end of a large pool."""
+    B = binding()
+    st = state(1400, [500, 333], 32, 8)
+    window, wo32 = window_decode(st, 200, 70)
+    sums = torch.zeros(2, 8, st.page_table.shape[1] * 64, device="cuda")
+    full, _ = weights_decode(st, sums)
+    small, n = st.kv, 66000                                      # 66000 x 8 x 8192 bytes of V
+    used = small.num_pages
+    big = B.PagedKV(*(torch.empty(n, *t.shape[1:], dtype=t.dtype, device="cuda") for t in (small.k_codes, small.k_sf, small.v_fp8, small.delta)),
+                    n, 32, 8)
+    for new, old in ((big.k_codes, small.k_codes), (big.k_sf, small.k_sf), (big.v_fp8, small.v_fp8), (big.delta, small.delta)):
+        new[n - used:] = old
+    st.kv, st.page_table = big, torch.where(st.page_table >= 0, st.page_table + (n - used), st.page_table)
+    assert torch.equal(window_decode(st, 200, 70)[0], window)
+    again = torch.zeros_like(sums)
+    assert torch.equal(weights_decode(st, again)[0], full) and torch.equal(again, sums)
+    new_table = torch.arange(n - used - 10, n - used, dtype=torch.int32, device="cuda").view(2, 5)
+    kept, new_lens, _, status = evict(big, st.page_table, st.seq_lens, sums, 300, 4, 32, new_table)
+    assert status == 0 and new_lens.tolist() == [300, 300]
+    for b in range(2):
+        old = [logical(big, int(p)) for p in st.page_table[b, :-(-int(st.seq_lens[b]) // 64)]]
+        k, s, v, d = logical(big, int(new_table[b, 4]))
+        for hk in range(8):
+            for i, a in enumerate(kept[b, hk, 256:].tolist()):
+                assert np.array_equal(v[hk, i], old[a // 64][2][hk, a % 64]) and np.array_equal(k[hk, i], old[a // 64][0][hk, a % 64])
+                assert np.array_equal(s[hk, i], old[a // 64][1][hk, a % 64]) and d[hk * 4 + 3, i] == old[a // 64][3][hk * 4 + 3, a % 64]
+    q4 = B.Fp4Tensor.empty(2, 32, 40)
+    B.mpfa_quantize_qk(torch.randn(2, 40, 32, 128, generator=torch.Generator().manual_seed(4)).bfloat16().cuda(), None,
+                       B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    outs = []
+    for kv, table in ((small, torch.where(st.page_table >= 0, st.page_table - (n - used), st.page_table)), (big, st.page_table)):
+        o = torch.empty(2, 40, 32, 128, dtype=torch.bfloat16, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.mpfa_prefill_paged_window(q4, kv, table, st.seq_lens, st.stats, 1.0, 100, 9, st.softmax_scale, o, None, status)
+        assert int(status) == 0
+        outs.append(o)
+    assert torch.equal(*outs)
