@@ -63,20 +63,26 @@ constexpr int LAUNCH_REGS = 96;
 // With runs (RUNS; the kernel alone, us, 16384 x 32 / 131072 x 32 / chunks of 512 on pages / 16384 x 32 from pages): 144/56/88/48 1553,
 // 96.6 ms, 310, 1720; 152/48/80/48 1556, 96.4 ms, 312, 1742; 144/48/88/56 1549, 97.0 ms, 315, 1737; 144/48/80/64 1564, 97.1 ms, 314,
 // 1752; 152/48/72/56 1598, 96.7 ms, 318, 1771.
-template <bool PAGED, bool LONG, bool RUNS> constexpr int REGS_EXP = RUNS ? (LONG && !PAGED ? 152 : 144) : (PAGED ? 152 : 144);
-template <bool PAGED, bool LONG, bool RUNS> constexpr int REGS_MAX = RUNS ? (LONG && !PAGED ? 48 : 56) : (PAGED || !LONG ? 48 : 56);
-template <bool PAGED, bool LONG, bool RUNS> constexpr int REGS_CORR = RUNS ? (LONG && !PAGED ? 80 : 88) : (PAGED || LONG ? 72 : 80);
-template <bool PAGED, bool LONG, bool RUNS> constexpr int REGS_UTIL = RUNS ? 48 : (PAGED ? 56 : 64);
-template <bool PAGED, bool LONG, bool RUNS>
+// Windows (the maximum warps make masks of their own; us, contiguous, 4001 tokens under 1024 / 16384 under 1024 / 16384 under 4096, 32:8
+// heads): 144/64/80/48 72.6, 298, 762; 144/56/80/56 72.8, 300, 765; 144/48/88/56 73.4, 302, 763; 144/56/88/48 72.9, 300, 765; 152/48/72/56
+// 72.7, 301, 799; 136/56/88/64 77.0, 319, 871.  On pages (chunks of 512, windows of 2048 / 4096): 144/64/80/48 95.7, 161; 144/56/80/56 95.6,
+// 165; 144/56/88/48 97.2, 163; 144/48/88/56 99.0, 171.
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false> constexpr int REGS_EXP = WINDOW ? 144 : RUNS ? (LONG && !PAGED ? 152 : 144) : (PAGED ? 152 : 144);
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false> constexpr int REGS_MAX = WINDOW ? 64 : RUNS ? (LONG && !PAGED ? 48 : 56) : (PAGED || !LONG ? 48 : 56);
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false> constexpr int REGS_CORR = WINDOW ? 80 : RUNS ? (LONG && !PAGED ? 80 : 88) : (PAGED || LONG ? 72 : 80);
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false> constexpr int REGS_UTIL = WINDOW ? 48 : RUNS ? 48 : (PAGED ? 56 : 64);
+template <bool PAGED, bool LONG, bool RUNS, bool WINDOW = false>
 constexpr bool regs_ok() {
-  constexpr int e = REGS_EXP<PAGED, LONG, RUNS>, m = REGS_MAX<PAGED, LONG, RUNS>, c = REGS_CORR<PAGED, LONG, RUNS>, u = REGS_UTIL<PAGED, LONG, RUNS>;
+  constexpr int e = REGS_EXP<PAGED, LONG, RUNS, WINDOW>, m = REGS_MAX<PAGED, LONG, RUNS, WINDOW>, c = REGS_CORR<PAGED, LONG, RUNS, WINDOW>,
+                u = REGS_UTIL<PAGED, LONG, RUNS, WINDOW>;
   // the exponent warps take registers (setmaxnreg.inc: not below the launch's), the others give them back (setmaxnreg.dec: not
   // above the launch's, or the instruction is illegal)
   return 8 * e + 4 * (m + c + u) <= 20 * LAUNCH_REGS && e >= LAUNCH_REGS && m <= LAUNCH_REGS && c <= LAUNCH_REGS && u <= LAUNCH_REGS &&
          u >= 24 && e % 8 == 0 && m % 8 == 0 && c % 8 == 0 && u % 8 == 0;
 }
 static_assert(regs_ok<false, false, false>() && regs_ok<false, false, true>() && regs_ok<false, true, true>() && regs_ok<true, true, false>() &&
-              regs_ok<true, true, true>(), "setmaxnreg split");
+              regs_ok<true, true, true>() && regs_ok<false, false, false, true>() && regs_ok<false, false, true, true>() &&
+              regs_ok<true, true, false, true>() && regs_ok<true, true, true, true>(), "setmaxnreg split");
 
 enum {
   BAR_Q_FULL = 0,                       // [2] query tile of work item i in buffer i & 1
@@ -296,7 +302,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   uint32_t gb = 0;   // KV blocks of the items already walked
   uint32_t ti = 0;   // index of the current item in this CTA's list
 
-  if (warp < 4) setmaxnreg_dec<REGS_UTIL<PAGED, LONG, RUNS>>();
+  if (warp < 4) setmaxnreg_dec<REGS_UTIL<PAGED, LONG, RUNS, WINDOW>>();
   if (warp == 0) {
     // =========================== TMA producer ===========================
     // The whole warp runs the loop (uniform control flow keeps addresses and barrier handles in
@@ -489,7 +495,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
   } else if (warp >= 12 && warp < 16) {
     // =========================== running maximum ===========================
-    setmaxnreg_dec<REGS_MAX<PAGED, LONG, RUNS>>();
+    setmaxnreg_dec<REGS_MAX<PAGED, LONG, RUNS, WINDOW>>();
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     float *s_m = reinterpret_cast<float *>(smem + OFF_M);
@@ -545,7 +551,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
   } else if (warp >= 4 && warp < 12) {
     // =========================== exponentials ===========================
-    setmaxnreg_inc<REGS_EXP<PAGED, LONG, RUNS>>();
+    setmaxnreg_inc<REGS_EXP<PAGED, LONG, RUNS, WINDOW>>();
     const int grp = (warp - 4) >> 2;   // takes the KV blocks whose running count has this parity
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
@@ -642,7 +648,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
   } else if (warp >= 16) {
     // =========================== correction + epilogue ===========================
-    setmaxnreg_dec<REGS_CORR<PAGED, LONG, RUNS>>();
+    setmaxnreg_dec<REGS_CORR<PAGED, LONG, RUNS, WINDOW>>();
     const int row = (warp & 3) * 32 + lane;
     const float *s_m = reinterpret_cast<const float *>(smem + OFF_M);
     uint4 *const s_run = reinterpret_cast<uint4 *>(smem + OFF_RUN<PAGED>) + row;   // this thread's row: written and read by it alone
