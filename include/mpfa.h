@@ -343,6 +343,7 @@ mpfa_status mpfa_decode(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, c
  * A hidden token's K and Delta_S may hold anything.  Its V may in decode; in the prefill calls a NaN in V reaches every row of each query
  * tile that visits its block (mpfa_quantize_v writes one for a NaN in its input only).
  * Here a seq_lens[b] above 64 * max_pages_per_req is treated as that bound in decode too.
+ * Calls that overlap on the GPU need separate workspaces, as for mpfa_decode.
  * Partitions of mpfa_decode_window are 1024 keys of the blocks that are not left out, so its workspace follows the window:
  * mpfa_decode_window_workspace_bytes().  max_pages_per_req (and new_max_pages) of this section's calls is at most 2^24, a seq_lens[b] below 0 counts as 0. */
 mpfa_status mpfa_prefill_window(const mpfa_fp4_tensor *h_q, const mpfa_fp4_tensor *h_k, const uint8_t *v_fp8,
@@ -362,7 +363,7 @@ mpfa_status mpfa_decode_window(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *
  * the softmax weights before P is rounded, in FP32.  weights is [B, H_kv, weights_stride] FP32 with weights_stride >= 64 *
  * max_pages_per_req (else MPFA_ERR_INVALID_ARG); entries from seq_lens[b] on are left as they are.  A caller starts a token's sum at 0.
  * The output is mpfa_decode's.  seq_lens[b] above 64 * max_pages_per_req is treated as that bound.  The workspace also holds the logits:
- * mpfa_decode_weights_workspace_bytes(). */
+ * mpfa_decode_weights_workspace_bytes(); calls that overlap on the GPU need separate ones, and separate sums. */
 mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, const int32_t *page_table,
                                 int max_pages_per_req, const int32_t *seq_lens, const mpfa_stats *h_stats, float v_scale,
                                 float softmax_scale, float *weights, int weights_stride, void *out_bf16, float *out_f32,

@@ -1332,17 +1332,17 @@ extern "C" mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *q, const mpfa_
   // a block for each chunk of keys where that is a few waves of blocks or less
   const int chunks = (slots + W_KEYS - 1) / W_KEYS, some = (16 * n_sm - 1) / (p.B * p.H_kv) + 1;
   const dim3 grid((unsigned)(chunks < some ? chunks : some), (unsigned)p.H_kv, (unsigned)p.B);
-  void (*sums)(const DecodeParams, float *, size_t) = nullptr;
+  void (*kern)(const DecodeParams, float *, size_t) = nullptr;
   switch (p.H_q / p.H_kv) {
-    case 1: sums = decode_weights_kernel<1>; break;
-    case 2: sums = decode_weights_kernel<2>; break;
-    case 3: sums = decode_weights_kernel<3>; break;
-    case 4: sums = decode_weights_kernel<4>; break;
-    case 5: sums = decode_weights_kernel<5>; break;
-    case 6: sums = decode_weights_kernel<6>; break;
-    case 7: sums = decode_weights_kernel<7>; break;
-    default: sums = decode_weights_kernel<8>; break;
+    case 1: kern = decode_weights_kernel<1>; break;
+    case 2: kern = decode_weights_kernel<2>; break;
+    case 3: kern = decode_weights_kernel<3>; break;
+    case 4: kern = decode_weights_kernel<4>; break;
+    case 5: kern = decode_weights_kernel<5>; break;
+    case 6: kern = decode_weights_kernel<6>; break;
+    case 7: kern = decode_weights_kernel<7>; break;
+    default: kern = decode_weights_kernel<8>; break;
   }
-  MPFA_CUDA_OK(launch(sums, grid, dim3(W_THREADS), 0, s, p, weights, (size_t)weights_stride));
+  MPFA_CUDA_OK(launch(kern, grid, dim3(W_THREADS), 0, s, p, weights, (size_t)weights_stride));
   return MPFA_OK;
 }

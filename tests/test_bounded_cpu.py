@@ -153,6 +153,11 @@ def test_the_plain_statement_is_the_oracles():
             assert (np.abs(np.stack([got[h, i] for i in pos]) - want) <= room).all()
 
 
+def test_the_launch_rule_covers_the_kernels():
+    from test_launch_rule import launched
+    assert {"decode_weights_kernel", "evict_select_kernel", "evict_move_kernel"} <= launched()
+
+
 def test_the_plain_visibility_by_hand():
     assert plain.visible([5], 8, 2, 1).astype(int).tolist() == [[1, 0, 0, 0, 1, 1, 0, 0]]
     assert plain.visible([0, -1], 2, 1, 2).astype(int).tolist() == [[1, 0], [0, 0]]
