@@ -1,6 +1,7 @@
 // Eviction from the paged cache by accumulated attention weight, for sm_100a: two kernels, neither with any arithmetic on the tokens.
 //
-// evict_select_kernel, one CTA per (request, kv head).  Of n > keep tokens the first `sinks` and the last `recent` stay; of the others
+// evict_select_kernel, one CTA per row of weights (request, kv head), or where rows are long and few a cluster: each CTA takes a part of the
+// slots, its histogram's counts are added up by all of them, a part of the bins each, and the first ranks the list.  Of n > keep tokens the first `sinks` and the last `recent` stay; of the others
 // the need = keep - sinks - recent with the largest 64-bit keys: the weight as the 32-bit integer that compares like it (-0 as +0, NaN
 // below everything), then the slot's complement.  No two keys are equal, so what is kept is what is not below the need-th largest.
 // It is found by digits of 12 bits from the top: a histogram of the candidates that agree with the digits so far, and the bin in which the
@@ -10,7 +11,9 @@
 // in shared memory, or in L2 where there are more than fit.
 // Bound by instructions and by barriers of 32 warps, not by memory: 8 heads of 4608 weights 8 us, 256 of 4200..9000 18 us (two CTAs to an
 // SM, 74 % of issue slots).  Not kept: three digits to the end and two scans of the block (25 us; 512 or 256 threads 16 us for the 8 heads),
-// copies of the histogram by lane (no gain: 60 bins hold most counts, but the conflicts are not what it waits for).
+// copies of the histogram by lane (no gain: 60 bins hold most counts, but the conflicts are not what it waits for).  One CTA to a row of 131072
+// weights: the whole call 164 us, by eight 30.5 (the rule and more figures stand at the launch; a row that is short in a wide table pays 3 us
+// for the cluster).
 //
 // evict_move_kernel, one CTA per (new page, kv head, request): the 64 tokens of the page from their slots.  A token's K codes, scales,
 // V and Delta_S entries are whole 16-, 8- and 2-byte pieces in every slot, whose places depend on the slot (include/mpfa.h), so the new
@@ -44,6 +47,7 @@ constexpr int DIGIT = 12, BINS = 1 << DIGIT;
 constexpr int LIST = SEL_THREADS / 4;   // ranked against one another by four threads each
 constexpr int SEL_CACHE = 49152;   // weights held in shared memory between the passes: 192 KB
 constexpr int SEL_AHEAD = 4;       // loads of a thread on the way
+constexpr int SEL_ALONE = 16384, SEL_PART = 4096;   // slots that the longest row can have: for one CTA; for each of several, at least
 
 __device__ __forceinline__ uint32_t order_of(float w) {
   if (w != w) return 0u;
@@ -58,22 +62,49 @@ __device__ __forceinline__ uint32_t before_warp(const uint32_t *tmp) {
   return __reduce_add_sync(0xffffffffu, lane < (int)(threadIdx.x >> 5) ? tmp[lane] : 0u);
 }
 
+constexpr int SEL_CLUSTER = 8;
 struct SelectShared {
   union {   // the list is made when the last histogram has been read
     __align__(16) uint32_t hist[BINS];
-    uint64_t list[LIST];
+    uint64_t list[LIST];        // the first CTA's
   };
   uint32_t tmp[2][SEL_WARPS], bin, need, inside, listed;
+  uint32_t total[SEL_CLUSTER], stay[SEL_CLUSTER];   // each CTA's candidates in its part of the bins; its slots that stay
   uint64_t border;
 };
 
-// The slots kept of n > keep, to kept[] in ascending order.  HELD: `held` has the orders of all weights, and sh.hist the counts of the
-// candidates' first digits; otherwise both are made from the weights w in global memory.
-template <bool HELD>
-__device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32_t *held, const float *w, int n, int32_t *kept, SelectShared &sh) {
+// The CTAs that share a row: C of them, this one the r-th.  One: shared memory and barriers of its own.
+template <bool CLUSTER>
+struct Team {
+  int C, r;
+  __device__ __forceinline__ void sync() const {   // writes to shared memory, the others' included, are seen after it
+    if (CLUSTER) {
+      __syncwarp();
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void tell(T &x, T value) const {   // one thread: the variable in every CTA
+    if (CLUSTER) {
+      for (int q = 0; q < C; ++q) cluster_store(cluster_address(smem_u32(&x), q), value);
+    } else {
+      x = value;
+    }
+  }
+};
+
+// This CTA's part [begin, end) of a row of n > keep slots: those that stay, to kept[] in ascending order.  HELD: `held` has the orders of the
+// part's weights (from held[0] on), and sh.hist the counts of its candidates' first digits; otherwise both are made from the weights w in
+// global memory.
+template <bool CLUSTER, bool HELD>
+__device__ __forceinline__ void select_tokens(const EvictParams &p, const Team<CLUSTER> &team, const uint32_t *held, const float *w, int n, int begin,
+                                              int end, int32_t *kept, SelectShared &sh) {
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const int first = p.sinks, last = n - p.recent;   // the candidates: [first, last)
-  auto order = [&](int i) { return HELD ? held[i] : order_of(w[i]); };
+  const int first = max(p.sinks, begin), last = min(n - p.recent, end);   // the part's candidates: [first, last)
+  auto order = [&](int i) { return HELD ? held[i - begin] : order_of(w[i]); };
   uint32_t need = (uint32_t)(p.keep - p.sinks - p.recent);
   uint32_t least = 0xffffffffu;   // no weight has this order
   int slot = -1;                  // of those of the least order, the last that stays
@@ -83,13 +114,13 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32
     int shift = 32;
     bool by_slot = false, counted = HELD;
 #pragma unroll 1
-    for (uint32_t inside = (uint32_t)(last - first); inside > LIST; counted = false) {
+    for (uint32_t inside = (uint32_t)(n - p.recent - p.sinks); inside > LIST; counted = false) {
       if (shift == 0) shift = 32, by_slot = true;
       const int bits = min(DIGIT, shift);
       shift -= bits;
       const uint32_t digit = (1u << bits) - 1u;
       if (!counted) {
-        __syncthreads();   // of the pass before: bin, need, inside and the histogram have been read
+        __syncthreads();   // of the pass before: bin, need and inside have been read, and the histogram before that
         reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
 #pragma unroll 2
@@ -98,14 +129,38 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32
           if ((u & mask) == value && (s & s_mask) == s_value) atomicAdd(&sh.hist[((by_slot ? s : u) >> shift) & digit], 1u);
         }
       }
-      __syncthreads();
-      // four bins to a lane, the highest first: the warp, then the lane and the bin in which the count from above reaches `need`
-      static_assert(BINS == 4 * SEL_THREADS, "four bins to a thread");
-      const uint4 c4 = reinterpret_cast<const uint4 *>(sh.hist)[SEL_THREADS - 1 - t];
-      const uint32_t c[4] = {c4.w, c4.z, c4.y, c4.x}, sum = (c[0] + c[1]) + (c[2] + c[3]), total = __reduce_add_sync(0xffffffffu, sum);
+      team.sync();
+      // Each CTA takes its part of the bins, the highest first, four to a lane or fewer, adds up what all CTAs have there and tells the others
+      // the sum; the part, the warp, the lane and the bin are found in which the count from above reaches `need`.
+      static_assert(BINS == 4 * SEL_THREADS, "at most four bins to a thread");
+      uint32_t c[4] = {0u, 0u, 0u, 0u};
+      int top;   // the thread's highest bin
+      if (CLUSTER) {
+        const int part = BINS / team.C, per = max(part / SEL_THREADS, 1);
+        top = BINS - 1 - team.r * part - t * per;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (u < per && t * per < part) {
+            const uint32_t at = smem_u32(&sh.hist[top - u]);
+            for (int q = 0; q < team.C; ++q) c[u] += cluster_load(cluster_address(at, q));
+          }
+      } else {
+        top = BINS - 1 - 4 * t;
+        const uint4 c4 = reinterpret_cast<const uint4 *>(sh.hist)[SEL_THREADS - 1 - t];
+        c[0] = c4.w, c[1] = c4.z, c[2] = c4.y, c[3] = c4.x;
+      }
+      const uint32_t sum = (c[0] + c[1]) + (c[2] + c[3]), total = __reduce_add_sync(0xffffffffu, sum);
       if (lane == 0) sh.tmp[0][warp] = total;
       __syncthreads();
       uint32_t above = before_warp(sh.tmp[0]);
+      if (CLUSTER) {
+        if (warp == 0) {
+          const uint32_t all = __reduce_add_sync(0xffffffffu, sh.tmp[0][lane]);
+          if (lane < team.C) cluster_store(cluster_address(smem_u32(&sh.total[team.r]), lane), all);
+        }
+        team.sync();
+        for (int q = 0; q < team.r; ++q) above += sh.total[q];
+      }
       if (above < need && need <= above + total) {
         uint32_t incl = sum;
 #pragma unroll
@@ -116,52 +171,58 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32
         above += incl - sum;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          if (above < need && need <= above + c[u]) sh.bin = (uint32_t)(BINS - 1 - 4 * t - u), sh.need = need - above, sh.inside = c[u];
+          if (above < need && need <= above + c[u]) team.tell(sh.bin, (uint32_t)(top - u)), team.tell(sh.need, need - above), team.tell(sh.inside, c[u]);
           above += c[u];
         }
       }
-      if (t == 0) sh.listed = 0;
-      __syncthreads();
+      team.sync();
       (by_slot ? s_value : value) |= sh.bin << shift;
       (by_slot ? s_mask : mask) |= digit << shift;
       need = sh.need, inside = sh.inside;
     }
-    // the candidates of that bin, in any order; the one with need - 1 larger ones is the last that stays
-    __syncthreads();
-    if (mask == 0) {   // no digit was needed
-      if (t == 0) sh.listed = 0;
-      __syncthreads();
-    }
+    // The candidates of that bin, in any order, on the first CTA; the one with need - 1 larger ones is the last that stays.
+    if (t == 0) sh.listed = 0;
+    team.sync();
 #pragma unroll 4
     for (int i = first + t; i < last; i += SEL_THREADS) {
       const uint32_t u = order(i), s = ~(uint32_t)i;
-      if ((u & mask) == value && (s & s_mask) == s_value) sh.list[atomicAdd(&sh.listed, 1u)] = (uint64_t)u << 32 | s;
+      if ((u & mask) == value && (s & s_mask) == s_value) {
+        const uint64_t key = (uint64_t)u << 32 | s;
+        if (CLUSTER) {
+          const uint32_t at = cluster_add(cluster_address(smem_u32(&sh.listed), 0), 1u);
+          cluster_store(cluster_address(smem_u32(&sh.list[0]), 0) + 8 * at, key);
+        } else {
+          sh.list[atomicAdd(&sh.listed, 1u)] = key;
+        }
+      }
     }
-    __syncthreads();
+    team.sync();
     // four threads to a candidate
-    const int m = (int)sh.listed;
-    if (warp * 8 < m) {
-      const uint64_t mine = (t >> 2) < m ? sh.list[t >> 2] : ~0ull;
-      uint32_t larger = 0;
+    if (!CLUSTER || team.r == 0) {
+      const int m = (int)sh.listed;
+      if (warp * 8 < m) {
+        const uint64_t mine = (t >> 2) < m ? sh.list[t >> 2] : ~0ull;
+        uint32_t larger = 0;
 #pragma unroll 4
-      for (int i = t & 3; i < m; i += 4) larger += sh.list[i] > mine ? 1u : 0u;
-      larger += __shfl_xor_sync(0xffffffffu, larger, 1);
-      larger += __shfl_xor_sync(0xffffffffu, larger, 2);
-      if ((t >> 2) < m && larger == need - 1) sh.border = mine;
+        for (int i = t & 3; i < m; i += 4) larger += sh.list[i] > mine ? 1u : 0u;
+        larger += __shfl_xor_sync(0xffffffffu, larger, 1);
+        larger += __shfl_xor_sync(0xffffffffu, larger, 2);
+        if ((t & 3) == 0 && (t >> 2) < m && larger == need - 1) team.tell(sh.border, mine);
+      }
     }
-    __syncthreads();
+    team.sync();
     least = (uint32_t)(sh.border >> 32), slot = (int)~(uint32_t)sh.border;
   }
-  // In the order of the slots: each warp takes a run of them, counts, and writes when it knows what the warps before it have.
-  const int run = ((n + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, begin = min(warp * run, n), end = min(begin + run, n);
+  // In the order of the slots: each warp takes a run of them, counts, and writes when it knows what is before it.
+  const int run = ((end - begin + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, from = min(begin + warp * run, end), until = min(from + run, end);
   auto stays = [&](int i) {
-    if (i >= end) return false;
+    if (i >= until) return false;
     const uint32_t u = order(i);
-    return i < first || i >= last || u > least || (u == least && i <= slot);
+    return i < p.sinks || i >= n - p.recent || u > least || (u == least && i <= slot);
   };
   uint32_t count = 0, answers = 0;   // of the first 32 groups of 32 slots lane k keeps the k-th answer
 #pragma unroll 2
-  for (int i0 = begin, k = 0; i0 < end; i0 += 32, ++k) {
+  for (int i0 = from, k = 0; i0 < until; i0 += 32, ++k) {
     const uint32_t bits = __ballot_sync(0xffffffffu, stays(i0 + lane));
     count += __popc(bits);
     if (k == lane) answers = bits;
@@ -169,58 +230,79 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const uint32
   if (lane == 0) sh.tmp[1][warp] = count;
   __syncthreads();
   uint32_t to = before_warp(sh.tmp[1]);
+  if (CLUSTER) {
+    if (p.keep == p.sinks + p.recent) team.sync();   // no other barrier has told that all CTAs are there
+    if (warp == 0) {
+      const uint32_t all = __reduce_add_sync(0xffffffffu, sh.tmp[1][lane]);
+      if (lane < team.C) cluster_store(cluster_address(smem_u32(&sh.stay[team.r]), lane), all);
+    }
+    team.sync();   // the last access to another CTA's memory is behind it
+    for (int q = 0; q < team.r; ++q) to += sh.stay[q];
+  }
 #pragma unroll 2
-  for (int i0 = begin, k = 0; i0 < end; i0 += 32, ++k) {
+  for (int i0 = from, k = 0; i0 < until; i0 += 32, ++k) {
     const uint32_t bits = k < 32 ? __shfl_sync(0xffffffffu, answers, k) : __ballot_sync(0xffffffffu, stays(i0 + lane));
     if (bits >> lane & 1u) kept[to + __popc(bits & ((1u << lane) - 1u))] = i0 + lane;
     to += __popc(bits);
   }
 }
 
-__global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t held[];          // the orders of the weights, where they fit
+// grid (C x kv heads, requests); the C CTAs of a row are a cluster.
+template <bool CLUSTER>
+__global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ EvictParams p, int C) {
+  extern __shared__ uint32_t held[];          // the orders of the part's weights, where they fit
   __shared__ SelectShared sh;
   grid_dependency_wait();
   launch_dependents();
-  const int hk = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
+  const Team<CLUSTER> team{CLUSTER ? C : 1, CLUSTER ? (int)blockIdx.x % C : 0};
+  const int hk = (int)blockIdx.x / team.C, b = blockIdx.y, t = threadIdx.x;
   const size_t head = (size_t)b * p.H_kv + hk;
   const float *const w = p.weights + head * p.weights_stride;
   int32_t *const kept = p.kept + head * p.keep;
   float *const out = p.new_weights + head * p.new_stride;
-  // the first weights are requested before the length is known: their slots exist whatever it is
+  // where the part begins at slot 0 whatever the length, its first weights are requested before that is known: their slots exist
   const int most = p.max_pages * PAGE;
   float x[SEL_AHEAD];
+  if (!CLUSTER) {
 #pragma unroll
-  for (int u = 0; u < SEL_AHEAD; ++u) x[u] = t + u * SEL_THREADS < most ? w[t + u * SEL_THREADS] : 0.0f;
+    for (int u = 0; u < SEL_AHEAD; ++u) x[u] = t + u * SEL_THREADS < most ? w[t + u * SEL_THREADS] : 0.0f;
+  }
   const int n = p.length(b), count = min(n, p.keep);
+  const int part = (n + team.C - 1) / team.C, begin = min(team.r * part, n), end = min(begin + part, n);
   reinterpret_cast<uint4 *>(sh.hist)[t] = make_uint4(0u, 0u, 0u, 0u);
-  if (hk == 0 && t == 0) p.new_lens[b] = count;
-  for (size_t i = (size_t)count + t; i < p.new_stride; i += SEL_THREADS) out[i] = 0.0f;
-  for (int i = count + t; i < p.keep; i += SEL_THREADS) kept[i] = -1;
+  if (hk == 0 && team.r == 0 && t == 0) p.new_lens[b] = count;
+  for (size_t i = (size_t)count + team.r * SEL_THREADS + t; i < p.new_stride; i += (size_t)team.C * SEL_THREADS) out[i] = 0.0f;
+  for (int i = count + team.r * SEL_THREADS + t; i < p.keep; i += team.C * SEL_THREADS) kept[i] = -1;
   if (n <= p.keep) {
-    for (int i = t; i < n; i += SEL_THREADS) kept[i] = i;
-  } else if (n <= SEL_CACHE) {
+    for (int i = begin + t; i < end; i += SEL_THREADS) kept[i] = i;
+  } else if (part <= SEL_CACHE) {
     __syncthreads();
 #pragma unroll 1
-    for (int i0 = t;;) {
+    for (int i0 = begin + t;;) {
+      if (CLUSTER) {
+#pragma unroll
+        for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i0 + u * SEL_THREADS < end ? w[i0 + u * SEL_THREADS] : 0.0f;
+      }
 #pragma unroll
       for (int u = 0; u < SEL_AHEAD; ++u) {
         const int i = i0 + u * SEL_THREADS;
-        if (i < n) {
+        if (i < end) {
           const uint32_t o = order_of(x[u]);
-          held[i] = o;
+          held[i - begin] = o;
           if (i >= p.sinks && i < n - p.recent) atomicAdd(&sh.hist[o >> (32 - DIGIT)], 1u);
         }
       }
       i0 += SEL_AHEAD * SEL_THREADS;
-      if (i0 >= n) break;
+      if (i0 >= end) break;
+      if (!CLUSTER) {
 #pragma unroll
-      for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i0 + u * SEL_THREADS < n ? w[i0 + u * SEL_THREADS] : 0.0f;
+        for (int u = 0; u < SEL_AHEAD; ++u) x[u] = i0 + u * SEL_THREADS < n ? w[i0 + u * SEL_THREADS] : 0.0f;
+      }
     }
     __syncthreads();
-    select_tokens<true>(p, held, w, n, kept, sh);
+    select_tokens<CLUSTER, true>(p, team, held, w, n, begin, end, kept, sh);
   } else {
-    select_tokens<false>(p, held, w, n, kept, sh);
+    select_tokens<CLUSTER, false>(p, team, held, w, n, begin, end, kept, sh);
   }
 }
 
@@ -357,10 +439,29 @@ extern "C" mpfa_status mpfa_evict_paged(const mpfa_paged_kv *kv, const int32_t *
   p.sinks = sinks;
   p.recent = recent;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // CTAs to a row.  One up to SEL_ALONE slots, more where an SM is free for each of them (two to an SM lose more than they gain, and clusters of
+  // eight leave SMs of a GPC over) and they have SEL_PART slots each; of a part of the device the driver says what fits.  One request, 32:8 heads,
+  // one CTA / as many as the rule says (us): 9000 slots 14.3 / 16.7 with two, 16384 18.8 / 18.8 with four, 32768 29.4 / 20.1, 65536 81.8 / 23.2,
+  // 131072 164 / 30.5; two of 20000 23.1 / 20.4 with four, 29.4 with eight; four of 32768 67.4 / 59.2 with four, 83.2 with eight; eight of
+  // 65536 115 / 65.3 with two, 75.9 with four; sixteen of 16384 62.9 / 78.1 with two.
   const int most = max_pages_per_req * PAGE;   // no request is longer
-  const size_t smem = (size_t)(most <= SEL_CACHE ? most : SEL_CACHE) * sizeof(uint32_t);
-  if ((rc = allow_smem<evict_select_kernel>(smem)) != MPFA_OK) return rc;
-  MPFA_CUDA_OK(launch(evict_select_kernel, dim3((unsigned)p.H_kv, (unsigned)B), dim3(SEL_THREADS), smem, s, p));
+  int C = SEL_CLUSTER;
+  while (C > 1 && (most <= SEL_ALONE || most < C * SEL_PART || (C < 8 ? (int64_t)heads * C > n_sm : (int64_t)heads * C * 3 > 2 * n_sm))) C /= 2;
+  const auto bytes = [&](int c) {
+    const int part = (most + c - 1) / c;
+    return (size_t)(part <= SEL_CACHE ? part : SEL_CACHE) * sizeof(uint32_t);
+  };
+  const auto grid = [&](int c) { return Grid(dim3((unsigned)(c * p.H_kv), (unsigned)B), (unsigned)c); };
+  if (C > 1) {
+    if ((rc = allow_smem<evict_select_kernel<true>>(bytes(2))) != MPFA_OK) return rc;
+    while (C > 1 && max_active_clusters(evict_select_kernel<true>, grid(C), dim3(SEL_THREADS), bytes(C), s) < 1) C /= 2;
+  }
+  if (C > 1) {
+    MPFA_CUDA_OK(launch(evict_select_kernel<true>, grid(C), dim3(SEL_THREADS), bytes(C), s, p, C));
+  } else {
+    if ((rc = allow_smem<evict_select_kernel<false>>(bytes(1))) != MPFA_OK) return rc;
+    MPFA_CUDA_OK(launch(evict_select_kernel<false>, grid(1), dim3(SEL_THREADS), bytes(1), s, p, 1));
+  }
   const int pages = (keep + PAGE - 1) / PAGE;
   MPFA_CUDA_OK(launch(evict_move_kernel, dim3((unsigned)(pages < max_pages_per_req ? pages : max_pages_per_req), (unsigned)p.H_kv, (unsigned)B),
                       dim3(MOVE_THREADS), 0, s, p));

@@ -91,6 +91,19 @@ __device__ __forceinline__ void cluster_store(uint32_t addr, double x) {
 __device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t x) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory");
 }
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint64_t x) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(x) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_load(uint32_t addr) {
+  uint32_t x;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+  return x;
+}
+__device__ __forceinline__ uint32_t cluster_add(uint32_t addr, uint32_t x) {   // what was there before
+  uint32_t old;
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(addr), "r"(x) : "memory");
+  return old;
+}
 
 // ---------------------------------------------------------------- TMA
 // 2D tiled load global -> shared, completion counted in bytes on `bar`.

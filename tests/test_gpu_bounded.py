@@ -457,7 +457,7 @@ def test_eviction_without_delta_and_with_spare_columns():
 
 
 @pytest.mark.parametrize("kind", ["equal", "two", "zeros", "special", "dense", "negative"])
-@pytest.mark.parametrize("L", [200, 5000, 60000])
+@pytest.mark.parametrize("L", [200, 5000, 20000, 60000])   # rows of one CTA, and of clusters of four and eight
 def test_eviction_by_weights_that_are_alike(kind, L):
     """Ties, the lowest slot first; infinities and NaN; many weights that differ in their last bits only; more than fit shared memory."""
     keep, sinks, recent = L // 2 + 1, 3, 10
@@ -824,3 +824,44 @@ def test_pools_of_more_than_four_gigabytes():
         assert int(status) == 0
         outs.append(o)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("nb,H_kv,L,keep,sinks,recent,kind", [
+    (1, 2, 400000, 1000, 4, 100, "rand"),         # a cluster's parts do not fit shared memory
+    (1, 1, 400000, 399000, 0, 0, "equal"),
+    (75, 2, 49300, 600, 1, 64, "rand"),           # too many rows for clusters, too long for shared memory
+    (80, 2, 20000, 8000, 10, 5, "two"),           # too many rows for clusters
+    (30, 2, 20000, 8000, 10, 5, "rand"),          # clusters of two
+    (1, 1, 20000, 5000, 2000, 3000, "rand"),      # clusters, protected tokens only
+    (1, 3, 20000, 19999, 7, 7, "rand"),
+    (2, 2, 33000, 1, 0, 0, "equal"),
+])
+def test_eviction_of_long_rows(nb, H_kv, L, keep, sinks, recent, kind):
+    """Rows that several CTAs share, or that do not fit where they are held; lengths differ within a batch, short ones and none among them.
+    Tables share the source pages (they are only read)."""
+    B = binding()
+    pages, per = -(-L // 64), -(-keep // 64)
+    kv = B.PagedKV(*(torch.zeros(pages + nb * per, H_kv, n, dtype=torch.uint8, device="cuda") for n in (4096, 512, 8192)), None, pages + nb * per, H_kv,
+                   H_kv)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(nb, 1)
+    new_table = torch.arange(pages, pages + nb * per, dtype=torch.int32, device="cuda").view(nb, per)
+    g = torch.Generator().manual_seed(L + keep)
+    w = torch.rand(nb, H_kv, pages * 64, generator=g)
+    if kind == "equal":
+        w.fill_(1.0)
+    elif kind == "two":
+        w = (w > 0.5).float()
+    w = w.cuda()
+    lens = [L if b % 4 == 0 else (0, keep, min(L, keep + 700))[b % 3] for b in range(nb)]
+    got = evict(kv, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), w, keep, sinks, recent, new_table)
+    assert got[3] == 0 and got[1].tolist() == [min(n, keep) for n in lens]
+    for b in sorted({0, 1 % nb, 2 % nb, 3 % nb, nb - 1}):
+        for hk in range(H_kv):
+            want = plain.evicted(w[b, hk].cpu().numpy(), lens[b], keep, sinks, recent)
+            assert np.array_equal(got[0][b, hk, :len(want)].cpu().numpy(), want), (b, hk)
+            assert (got[0][b, hk, len(want):] == -1).all() and not got[2][b, hk, len(want):].any()
+            assert np.array_equal(got[2][b, hk, :len(want)].cpu().numpy(), w[b, hk].cpu().numpy()[want])
+    # every row is as long as its count says, ascending
+    rows, n = got[0], torch.tensor([min(x, keep) for x in lens], device="cuda").view(-1, 1, 1)
+    live = torch.arange(keep, device="cuda") < n
+    assert bool(((rows >= 0) == live).all()) and bool(((rows[..., 1:] > rows[..., :-1]) | ~live[..., 1:]).all())
