@@ -57,13 +57,14 @@
 // (mpfa_decode_weights).
 //
 // Window.  Visible are the keys j >= L - window and j < sinks.  Keys are counted as if the 128-key blocks between the two ranges did not
-// exist (struct Span); only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor
+// exist (struct Span), by all roles alike, L too; only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor
 // copied, so its table entry may be stale, and of the V rows of a page that is visible in part the others are zeros: a hidden token's V may
 // be anything, NaN included, and 0 x NaN is not 0.
 // Whole calls back to back: one request under a window of 1024 13.9 us (two kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
-// of cache) 89 us, 4.7 TB/s; 32 under 16384 (0.88 GB) 150 us, 5.9 TB/s.  Windows rarely end with a partition, so one item in five of the
-// 64 requests has one or two blocks, and such an item costs 2 us whatever it holds (instruction fetch: 2.0 stalled warps per issue for
-// want of an instruction, 0.6 where all items are long).  Masks made from tokens' own indices, with the block looked up for every one: 91.4.
+// of cache) 87 us, 4.8 TB/s; 32 under 16384 (0.88 GB) 149 us, 5.9 TB/s.  Windows rarely end with a partition, so one item in five of the
+// 64 requests has one or two blocks, and such an item costs a microsecond more than its bytes do, by instruction fetch (2.0 stalled warps per
+// issue for want of an instruction, 0.6 where all items are long).  So what a role adds counts: masks made from tokens' own indices 91.4,
+// with the window's bounds carried in every role's item 89.5; page ids of the item after a short one requested ahead 97.
 //
 // Weights.  The logits stay in FP32: 4 G bytes per key written, and read back by decode_weights_kernel once the merge has the (m, l) of the
 // whole request; recomputing them instead would read K, its scales and Delta_S again (72 + 2 G).  One request of 4097 keys 15.6 us (mpfa_decode
@@ -113,8 +114,8 @@ constexpr uint32_t D_OFF_MISC = D_OFF_XL + 2 * 8 * MAXG * 4;           // TMEM a
 constexpr int D_MAXREQ = 768;                                          // requests whose length / lambda are cached
 constexpr uint32_t D_OFF_LEN = D_OFF_MISC + 64;                        // [D_MAXREQ] int32 lengths
 constexpr uint32_t D_OFF_LAM = D_OFF_LEN + D_MAXREQ * 4;               // [D_MAXREQ] float
-constexpr uint32_t D_OFF_RING = D_OFF_LAM + D_MAXREQ * 4;              // [D_NITEM] int4 work items {b, hk, sp, L}
-constexpr uint32_t D_OFF_PRE = D_OFF_RING + D_NITEM * 16;              // [D_MAXREQ + 1] items of the requests before b
+constexpr uint32_t D_OFF_RING = D_OFF_LAM + D_MAXREQ * 4;              // [D_NITEM] int4 work items {b, hk, sp, L}, [D_NITEM] blocks left out
+constexpr uint32_t D_OFF_PRE = D_OFF_RING + D_NITEM * 20;              // [D_MAXREQ + 1] items of the requests before b
 constexpr uint32_t D_SMEM_USED = D_OFF_PRE + (D_MAXREQ + 4) * 4;
 constexpr uint32_t D_SMEM = D_SMEM_USED + 1024;     // slack for the 1024-byte alignment of the base
 
@@ -194,11 +195,9 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
-// The keys of a request as its work items count them: blocks [0, heads) are the sinks', then `shift` blocks are left out.
+// The keys of a request as its work items count them: without the `shift` blocks between those of the sinks and those of the window.
 struct Span {
-  int len;          // keys
-  int low;          // first key of the window; not below 128 heads, nor is `sinks` above that, where blocks are left out
-  int heads, shift; // 0, 0 where none are
+  int len, shift;
 };
 
 struct DecodeParams {
@@ -229,17 +228,18 @@ struct DecodeParams {
   }
   template <int MODE>
   __device__ __forceinline__ Span span(int L) const {
-    if constexpr (MODE != WINDOW) return Span{L, 0, 0, 0};
-    const int low = max(L - window, 0), heads = (min(sinks, low) + TILE - 1) / TILE, gap = max(low / TILE - heads, 0);
-    return Span{L - gap * TILE, low - gap * TILE, gap > 0 ? heads : 0, gap};
+    if constexpr (MODE != WINDOW) return Span{L, 0};
+    const int low = max(L - window, 0), gap = max(low / TILE - (min(sinks, low) + TILE - 1) / TILE, 0);
+    return Span{L - gap * TILE, gap};
   }
+  // partitions of that many keys as they are counted
+  __device__ __forceinline__ int n_parts(int len) const { return min((max(len, 0) + DECODE_SPLIT - 1) / DECODE_SPLIT, n_split); }
+  // First key of the window and whether a key is visible, all as they are counted: the window ends with the last key, and where blocks are
+  // left out none of the sinks is behind its first block.
+  __device__ __forceinline__ int low(int len) const { return max(len - window, 0); }
   template <int MODE>
-  __device__ __forceinline__ int n_parts(int L) const {
-    return min((max(span<MODE>(L).len, 0) + DECODE_SPLIT - 1) / DECODE_SPLIT, n_split);
-  }
-  template <int MODE>
-  __device__ __forceinline__ bool visible(const Span &sp, int key) const {
-    return key < sp.len && (MODE != WINDOW || key >= sp.low || key < sinks);
+  __device__ __forceinline__ bool visible(int key, int len) const {
+    return key < len && (MODE != WINDOW || key >= len - window || key < sinks);
   }
 };
 
@@ -293,33 +293,36 @@ struct DCtx {
 
 struct WorkIter {
   uint32_t n = 0;      // items taken so far
-  int b, hk, sp, L, nblk;
-  Span span;
+  int b, hk, sp, L, nblk;   // L: keys as they are counted
+  int shift;                // blocks that the count leaves out
   // Whole warp, or the one thread that stands for its warp.  false: no more items (or the CTA is giving up).
   template <int MODE, bool ONE_THREAD = false>
-  __device__ bool next(const DecodeParams &p, const DCtx &cx, const int4 *ring) {
+  __device__ bool next(const DCtx &cx, const int4 *ring) {
     const uint32_t slot = n % D_NITEM, parity = (n / D_NITEM) & 1;
     if (!(ONE_THREAD ? cx.wait(B_ITEM_FULL + slot, parity) : cx.wait_warp(B_ITEM_FULL + slot, parity))) return false;
     const int4 it = ring[slot];
     if (it.x < 0) return false;   // end marker: stays in its slot, nobody moves past it
+    shift = MODE == WINDOW ? reinterpret_cast<const int *>(ring + D_NITEM)[slot] : 0;
     if (ONE_THREAD)
       mbar_arrive(cx.bar(B_ITEM_EMPTY + slot));
     else
       cx.warp_arrive(B_ITEM_EMPTY + slot);
     ++n;
     b = it.x, hk = it.y, sp = it.z, L = it.w;
-    span = p.span<MODE>(L);
-    nblk = (min(span.len - sp * DECODE_SPLIT, DECODE_SPLIT) + TILE - 1) / TILE;
+    nblk = (min(L - sp * DECODE_SPLIT, DECODE_SPLIT) + TILE - 1) / TILE;
     return true;
   }
 };
 
 // Page ids of the blocks of one item, lane l holding block l's two table entries (loads only: the values
 // are range-checked where they are used, so that nothing waits for them here).
+template <int MODE>
 __device__ __forceinline__ void lookup_pages(const DecodeParams &p, const WorkIter &w, int lane, int &pid0, int &pid1) {
   pid0 = -1, pid1 = -1;
   if (lane < w.nblk) {
-    const int block = w.sp * MAXBLK + lane, pg = (block + (block >= w.span.heads ? w.span.shift : 0)) * (TILE / PAGE);
+    int block = w.sp * MAXBLK + lane;
+    if (MODE == WINDOW && block >= p.low(w.L) / TILE) block += w.shift;
+    const int pg = block * (TILE / PAGE);
     const int32_t *row = p.page_table + (size_t)w.b * p.max_pages;
     if (pg < p.max_pages) pid0 = row[pg];
     if (pg + 1 < p.max_pages) pid1 = row[pg + 1];
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       // pre[b] = items of requests 0..b-1: every lane sums a contiguous run of requests, the warp scans the runs
       const int per = (p.B + 31) / 32, lo = min(p.B, lane * per), hi = min(p.B, lo + per);
       int run = 0;
-      for (int i = lo; i < hi; ++i) run += p.n_parts<MODE>(len_tab[i]) * p.H_kv;
+      for (int i = lo; i < hi; ++i) run += p.n_parts(p.span<MODE>(len_tab[i]).len) * p.H_kv;
       int incl = run;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -440,7 +443,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       int acc = incl - run;
       for (int i = lo; i < hi; ++i) {
         pre[i] = acc;
-        acc += p.n_parts<MODE>(len_tab[i]) * p.H_kv;
+        acc += p.n_parts(p.span<MODE>(len_tab[i]).len) * p.H_kv;
       }
       total = (uint32_t)__shfl_sync(0xffffffffu, incl, 31);
       if (lane == 31) pre[p.B] = (int)total;
@@ -458,6 +461,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       if (ok && k >= (uint32_t)D_NITEM) ok = cx.wait_warp(B_ITEM_EMPTY + slot, ((k / D_NITEM) - 1) & 1);
       if (!ok) break;
       int4 item = make_int4(-1, 0, 0, 0);
+      int shift = 0;
       if (lane == 0) {
         for (bool first = k == 0;; first = false) {
           if (!first && !p.ticket) break;
@@ -469,19 +473,23 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
               const int mid = (lo + hi) >> 1;
               if ((uint32_t)pre[mid] <= tkt) lo = mid; else hi = mid;
             }
-            const int L = len_tab[lo], nsp = p.n_parts<MODE>(L);
-            const int r = (int)tkt - pre[lo];
-            item = make_int4(lo, r / nsp, r % nsp, L);
+            const Span keys = p.span<MODE>(len_tab[lo]);
+            const int nsp = p.n_parts(keys.len), r = (int)tkt - pre[lo];
+            item = make_int4(lo, r / nsp, r % nsp, keys.len);
+            shift = keys.shift;
             break;
           }
           const int sp = (int)(tkt % (uint32_t)p.n_split), r = (int)(tkt / (uint32_t)p.n_split);
-          const int b = r / p.H_kv, L = p.length<MODE>(b);
-          if (p.span<MODE>(L).len - sp * DECODE_SPLIT > 0) {
-            item = make_int4(b, r % p.H_kv, sp, L);
+          const int b = r / p.H_kv;
+          const Span keys = p.span<MODE>(p.length<MODE>(b));
+          if (keys.len - sp * DECODE_SPLIT > 0) {
+            item = make_int4(b, r % p.H_kv, sp, keys.len);
+            shift = keys.shift;
             break;
           }
         }
         ring_w[slot] = item;
+        if (MODE == WINDOW) reinterpret_cast<int *>(ring_w + D_NITEM)[slot] = shift;
         mbar_arrive(cx.bar(B_ITEM_FULL + slot));
       }
       item.x = __shfl_sync(0xffffffffu, item.x, 0);
@@ -489,7 +497,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       item.y = __shfl_sync(0xffffffffu, item.y, 0);
       item.z = __shfl_sync(0xffffffffu, item.z, 0);
       item.w = __shfl_sync(0xffffffffu, item.w, 0);
-      prev_short = p.span<MODE>(item.w).len - item.z * DECODE_SPLIT <= DECODE_SPLIT / 2;
+      prev_short = item.w - item.z * DECODE_SPLIT <= DECODE_SPLIT / 2;
       const size_t head0 = (size_t)item.x * p.H_q + (size_t)item.y * G;
       uint4 qv = make_uint4(0u, 0u, 0u, 0u);
       uint32_t qs0 = 0, qs1 = 0;
@@ -532,8 +540,8 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     const int b_full = is_k ? B_K_FULL : B_V_FULL, b_empty = is_k ? B_K_EMPTY : B_V_EMPTY;
     static_assert(D_NK % 2 == 0, "each K producer has its own stages");
     int pc0 = -1, pc1 = -1, pn0 = -1, pn1 = -1;
-    bool vw = w.next<MODE>(p, cx, ring), vn = false;
-    if (vw) lookup_pages(p, w, lane, pc0, pc1);
+    bool vw = w.next<MODE>(cx, ring), vn = false;
+    if (vw) lookup_pages<MODE>(p, w, lane, pc0, pc1);
     for (; ok && vw; ++j) {
       if (warp == 0) cx.warp_arrive(B_DRAW + (j & 1));
       // Nothing can be done with V before the first item's softmax, and while all CTAs start at once its copies only keep K waiting, of
@@ -541,13 +549,14 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       if (!is_k && j == 0) ok = cx.wait_warp(B_V_GO, 0);
       const int key0 = w.sp * DECODE_SPLIT + lane * TILE;
       const bool in = lane < w.nblk;
-      bool want0 = true, want1 = key0 + PAGE < w.span.len;
+      bool want0 = true, want1 = key0 + PAGE < w.L;
       // rows of the two pages between the sinks' end and the window's beginning: of a page that is all of it nothing is wanted, of another
       // one V takes these as zeros
       int hide0 = 0, show0 = 0, hide1 = 0, show1 = 0;
       if constexpr (MODE == WINDOW) {
-        hide0 = min(max(p.sinks - key0, 0), PAGE), show0 = min(max(w.span.low - key0, hide0), PAGE);
-        hide1 = min(max(p.sinks - key0 - PAGE, 0), PAGE), show1 = min(max(w.span.low - key0 - PAGE, hide1), PAGE);
+        const int low = p.low(w.L) - key0, sinks = p.sinks - key0;
+        hide0 = min(max(sinks, 0), PAGE), show0 = min(max(low, hide0), PAGE);
+        hide1 = min(max(sinks - PAGE, 0), PAGE), show1 = min(max(low - PAGE, hide1), PAGE);
         want0 = show0 - hide0 < PAGE, want1 = want1 && show1 - hide1 < PAGE;
       }
       const bool has0 = in && want0 && pc0 >= 0 && pc0 < p.num_pages, has1 = in && want1 && pc1 >= 0 && pc1 < p.num_pages;
@@ -579,7 +588,9 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
           if constexpr (MODE == WINDOW) {   // a token's V is one row of 128 bytes
             const int a0 = __shfl_sync(0xffffffffu, hide0, u), b0 = __shfl_sync(0xffffffffu, show0, u);
             const int a1 = __shfl_sync(0xffffffffu, hide1, u), b1 = __shfl_sync(0xffffffffu, show1, u);
+#pragma unroll 1
             for (int o = a0 * HEAD_DIM + lane * 16; o < b0 * HEAD_DIM; o += 512) *reinterpret_cast<uint4 *>(stage + o) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
             for (int o = a1 * HEAD_DIM + lane * 16; o < b1 * HEAD_DIM; o += 512)
               *reinterpret_cast<uint4 *>(stage + 8192 + o) = make_uint4(0u, 0u, 0u, 0u);
           } else {
@@ -627,8 +638,8 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         __syncwarp();
         if (t == max(0, w.nblk - 3)) {
           wn = w;
-          vn = wn.next<MODE>(p, cx, ring);
-          if (vn) lookup_pages(p, wn, lane, pn0, pn1);
+          vn = wn.next<MODE>(cx, ring);
+          if (vn) lookup_pages<MODE>(p, wn, lane, pn0, pn1);
         }
       }
       if (warp == 0 && j == 0) cx.warp_arrive(B_V_GO);
@@ -657,7 +668,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       WorkIter w;
       uint32_t kc = 0, j = 0;
       bool ok = true;
-      while (ok && w.next<MODE, true>(p, cx, ring)) {
+      while (ok && w.next<MODE, true>(cx, ring)) {
         const uint32_t par = j & 1;
         ok = cx.wait(B_Q_READY + par, (j >> 1) & 1);
         if (ok && j >= 2) ok = cx.wait(B_S_FREE + par, ((j >> 1) - 1) & 1);   // scores of item j-2 have been read
@@ -708,7 +719,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       WorkIter w;
       uint32_t vc = 0, j = 0;
       bool ok = true;
-      while (ok && w.next<MODE, true>(p, cx, ring)) {
+      while (ok && w.next<MODE, true>(cx, ring)) {
         const uint32_t par = j & 1;
         ok = cx.wait(B_P_READY + par, (j >> 1) & 1);
         if (ok && j >= 1) ok = cx.wait(B_O_FREE, (j - 1) & 1);   // the previous item's O has been read
@@ -739,7 +750,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     WorkIter w;
     uint32_t kc = 0;
     bool ok = true;
-    while (ok && w.next<MODE>(p, cx, ring)) {
+    while (ok && w.next<MODE>(cx, ring)) {
       for (int t = 0; t < w.nblk; ++t, ++kc) {
         const uint32_t st = kc % D_NK;
         ok = cx.wait_warp(B_K_FULL + st, (kc / D_NK) & 1);
@@ -766,7 +777,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     constexpr int GP = G <= 4 ? 4 : 8, TPV = 32 / GP, NV = MAXBLK / TPV;   // heads padded; blocks to a warp's lanes; such sets
     bool ok = true;
     WorkIter w;
-    for (uint32_t j = 0; ok && w.next<MODE>(p, cx, ring); ++j) {
+    for (uint32_t j = 0; ok && w.next<MODE>(cx, ring); ++j) {
       const uint32_t par = j & 1, ph = (j >> 1) & 1;
       const uint32_t tS = tm + TM_S + par * (MAXBLK * 16) + tlane;
       uint8_t *const pt = dsm + D_OFF_P + par * MAXBLK * 1024 + (r & 15);
@@ -792,7 +803,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         for (int u = 0; u < CH; ++u) {
           const int t = t0 + 2 * u;
           if (t < w.nblk) {
-            const bool valid = p.visible<MODE>(w.span, k_part + (w.nblk - 1 - t) * TILE + r);
+            const bool valid = p.visible<MODE>(k_part + (w.nblk - 1 - t) * TILE + r, w.L);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               const float wm = warp_max(valid ? __uint_as_float(sr[u][g]) : -INFINITY);
@@ -846,7 +857,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
           for (int u = 0; u < CH; ++u) {
             const int t = v * TPV + t0 + 2 * u;
             if (t < w.nblk) {
-              const bool valid = p.visible<MODE>(w.span, k_part + (w.nblk - 1 - t) * TILE + r);
+              const bool valid = p.visible<MODE>(k_part + (w.nblk - 1 - t) * TILE + r, w.L);
               float pq[G + 1];
               if constexpr (MODE == WEIGHTS) {
                 if (valid) {
@@ -895,7 +906,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
     const uint32_t tO = tm + TM_O + ((uint32_t)(quad * 32) << 16);
     bool ok = true;
     WorkIter w;
-    for (uint32_t j = 0; ok && w.next<MODE>(p, cx, ring); ++j) {
+    for (uint32_t j = 0; ok && w.next<MODE>(cx, ring); ++j) {
       const int par = j & 1;
       const float *wt = wtab + par * MAXBLK * MAXG, *xlg = xl + par * 8 * MAXG;
       ok = cx.wait_warp(B_P_READY + par, (j >> 1) & 1) && cx.wait_warp(B_O_FULL, j & 1);   // the item's tables; its accumulators
@@ -927,7 +938,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       cx.warp_arrive(B_O_FREE);
       cx.warp_arrive(B_T_FREE + par);
       const size_t head0 = (size_t)w.b * p.H_q + (size_t)w.hk * G;
-      const int n_parts = p.n_parts<MODE>(w.L);
+      const int n_parts = p.n_parts(w.L);
       if (n_parts == 1) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -990,7 +1001,7 @@ __global__ void __launch_bounds__(128, 9) decode_merge_kernel(const __grid_const
       x[u] = po[(size_t)s * (HEAD_DIM / 4)];
     }
   const float first_max = ml[min(lane, p.n_split - 1)].x;
-  const int n = p.n_parts<MODE>(p.length<MODE>(b));
+  const int n = p.n_parts(p.span<MODE>(p.length<MODE>(b)).len);
   const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
   if (n <= 1) return;
   float M = lane < n ? first_max : -INFINITY;
@@ -1051,7 +1062,7 @@ __global__ void __launch_bounds__(128) decode_merge_few_kernel(const __grid_cons
     a[s] = ml[at];
     x[s] = po[(size_t)at * (HEAD_DIM / 4)];
   }
-  const int n = p.n_parts<MODE>(p.length<MODE>(b));
+  const int n = p.n_parts(p.span<MODE>(p.length<MODE>(b)).len);
   const float lam = __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[b]), p.k_gscale[b]);
   if (n <= 1) return;
   float M = -INFINITY;

@@ -865,3 +865,35 @@ def test_eviction_of_long_rows(nb, H_kv, L, keep, sinks, recent, kind):
     rows, n = got[0], torch.tensor([min(x, keep) for x in lens], device="cuda").view(-1, 1, 1)
     live = torch.arange(keep, device="cuda") < n
     assert bool(((rows >= 0) == live).all()) and bool(((rows[..., 1:] > rows[..., :-1]) | ~live[..., 1:]).all())
+
+
+def test_eviction_of_long_rows_from_a_graph():
+    """The form with clusters captured and replayed on other weights and lengths than it was captured with."""
+    B = binding()
+    L, keep, H_kv = 33000, 5000, 2
+    pages, per = -(-L // 64), -(-keep // 64)
+    kv = B.PagedKV.empty(pages + per, H_kv, H_kv)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1)
+    new_table = torch.arange(pages, pages + per, dtype=torch.int32, device="cuda").view(1, -1)
+    w, lens = torch.rand(1, H_kv, pages * 64, device="cuda"), torch.tensor([L], dtype=torch.int32, device="cuda")
+    kept, new_lens = torch.empty(1, H_kv, keep, dtype=torch.int32, device="cuda"), torch.empty_like(lens)
+    new_weights, status = torch.empty(1, H_kv, keep, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def go():
+        B.mpfa_evict_paged(kv, table, lens, w, keep, 4, 100, new_table, kept, new_lens, new_weights, status)
+
+    go()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for n in (L, 21000, 5000, 17):
+        w.copy_(torch.rand(w.shape, generator=torch.Generator().manual_seed(n)))
+        lens.fill_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status) == 0 and new_lens.tolist() == [min(n, keep)]
+        for hk in range(H_kv):
+            want = plain.evicted(w[0, hk].cpu().numpy(), n, keep, 4, 100)
+            assert np.array_equal(kept[0, hk, :len(want)].cpu().numpy(), want)
+            assert np.array_equal(new_weights[0, hk, :len(want)].cpu().numpy(), w[0, hk].cpu().numpy()[want]) and not new_weights[0, hk, len(want):].any()
