@@ -409,7 +409,8 @@ extern "C" mpfa_status mpfa_evict_paged(const mpfa_paged_kv *kv, const int32_t *
       overlap(seq_lens, (size_t)B * sizeof(int32_t), new_lens, (size_t)B * sizeof(int32_t)))
     return MPFA_ERR_INVALID_ARG;
   if (!aligned(kv->k_codes, 256) || !aligned(kv->k_sf, 256) || !aligned(kv->v_fp8, 256) || !aligned(kv->delta_s_bf16, 256) ||
-      !aligned(weights, 4) || !aligned(new_weights, 4))
+      !aligned(weights, 4) || !aligned(new_weights, 4) || !aligned(page_table, 4) || !aligned(seq_lens, 4) || !aligned(new_table, 4) ||
+      !aligned(kept, 4) || !aligned(new_lens, 4))
     return MPFA_ERR_ALIGNMENT;
   int dev = 0, n_sm = 0;
   mpfa_status rc = device_info(&dev, &n_sm);

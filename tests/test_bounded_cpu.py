@@ -93,6 +93,7 @@ def test_evict_refusals(binding):
                          ({"kv": binding._PagedKV(A, A, A, A, 9, 64, 18, 2)}, -2), ({"kv": binding._PagedKV(A, A, A, A, 9, 64, 8, 3)}, -2),
                          ({"kv": binding._PagedKV(A, A, A, A, 0, 64, 8, 2)}, -1), ({"kv": binding._PagedKV(0, A, A, A, 9, 64, 8, 2)}, -1),
                          ({"kv": binding._PagedKV(A + 16, A, A, A, 9, 64, 8, 2)}, -3), ({"weights": 2 * A + 2}, -3), ({"B": 65536}, -2),
+                         ({"kept": A + 2}, -3), ({"new_lens": A + 65}, -3), ({"new_table": A + 1}, -3),
                          ({"pages": (1 << 24) + 1}, -2), ({"new_pages": (1 << 24) + 1}, -2)):
         assert call(binding, "mpfa_evict_paged", good, change) == want, change
 
