@@ -1,5 +1,8 @@
 """GPU: attention with a sliding window and sinks (prefill, chunks on pages, decode), decode that sums attention weights, and eviction,
 against the 64-bit statements of bounded_plain.py."""
+import contextlib
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -13,6 +16,16 @@ pytestmark = pytest.mark.gpu
 def binding():
     from paper_2609_33135_b200 import binding as B
     return B
+
+
+@contextlib.contextmanager
+def arrangement(a):
+    """The prefill calls' work arrangement; afterwards the one that the suite runs with."""
+    binding().mpfa_set_prefill_arrangement(a)
+    try:
+        yield
+    finally:
+        binding().mpfa_set_prefill_arrangement(int(os.environ.get("MPFA_TEST_ARRANGEMENT", "0")))
 
 
 def state(seed, lens, H_q, H_kv, v_scale=1.0, smooth=True):
@@ -198,7 +211,8 @@ def test_prefill_window(B_, N_q, N_kv, H_q, H_kv, window, sinks):
         check_rows(Q[b], K[b], V[b], D[b], o32[b].cpu().numpy(), pos, window, sinks, plain.lam_of(s1.stats, b, w.softmax_scale), 0.5,
                    (H_q, H_kv), b)
     if window >= N_kv:
-        full, f32, _ = B.prefill(s1, True, w.softmax_scale, want_f32=True)
+        with arrangement(0):
+            full, f32, _ = B.prefill(s1, True, w.softmax_scale, want_f32=True)
         assert torch.equal(full, out) and torch.equal(f32, o32)
 
 
@@ -208,16 +222,13 @@ def test_prefill_window_without_compensation_and_in_the_other_arrangement():
     w = wl.prefill_workload("pw", 970, 1, 500, 4, 2, True)
     s1 = B.stage1(w.q.cuda(), w.k.cuda(), w.v.cuda(), smooth=False)
     outs = []
-    for arrangement in (0, 1):
-        B.mpfa_set_prefill_arrangement(arrangement)
-        try:
+    for a in (0, 1):
+        with arrangement(a):
             o32 = torch.empty(1, 500, 4, 128, device="cuda")
             out = torch.empty(1, 500, 4, 128, dtype=torch.bfloat16, device="cuda")
             status = torch.zeros(1, dtype=torch.int32, device="cuda")
             B.mpfa_prefill_window(s1.q, s1.k, s1.v_fp8, None, s1.stats, 1.0, 150, 2, w.softmax_scale, out, o32, status)
             torch.cuda.synchronize()
-        finally:
-            B.mpfa_set_prefill_arrangement(0)
         assert int(status) == 0
         outs.append(o32)
     assert torch.equal(*outs)
