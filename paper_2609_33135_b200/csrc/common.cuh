@@ -96,7 +96,8 @@ mpfa_status device_info(int *dev, int *n_sm);
 constexpr int MAX_DEVICES = 64;
 
 // Lets a kernel use `bytes` of dynamic shared memory.  The driver keeps that per context, and a device can have several or lose one,
-// so it is told before every launch (no pass got measurably longer by it: one decode step 22.7 us without, 22.4 with).
+// so it is told before every launch (no pass got measurably longer by it: one decode step 22.7 us without, 22.4 with).  A kernel's bytes are
+// the same in every call: host threads launch side by side, and a lower number would hold for the others' launches too.
 template <auto Kernel>
 mpfa_status allow_smem(size_t bytes) {
   MPFA_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));

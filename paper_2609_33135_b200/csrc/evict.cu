@@ -452,15 +452,17 @@ extern "C" mpfa_status mpfa_evict_paged(const mpfa_paged_kv *kv, const int32_t *
     const int part = (most + c - 1) / c;
     return (size_t)(part <= SEL_CACHE ? part : SEL_CACHE) * sizeof(uint32_t);
   };
+  // What the kernel is allowed is the most that any call needs, since it holds for all of them: set to this call's own size, it would lower what
+  // another host thread has just set for a longer row, whose launch would be refused.
   const auto grid = [&](int c) { return Grid(dim3((unsigned)(c * p.H_kv), (unsigned)B), (unsigned)c); };
   if (C > 1) {
-    if ((rc = allow_smem<evict_select_kernel<true>>(bytes(2))) != MPFA_OK) return rc;
+    if ((rc = allow_smem<evict_select_kernel<true>>(SEL_CACHE * sizeof(uint32_t))) != MPFA_OK) return rc;
     while (C > 1 && max_active_clusters(evict_select_kernel<true>, grid(C), dim3(SEL_THREADS), bytes(C), s) < 1) C /= 2;
   }
   if (C > 1) {
     MPFA_CUDA_OK(launch(evict_select_kernel<true>, grid(C), dim3(SEL_THREADS), bytes(C), s, p, C));
   } else {
-    if ((rc = allow_smem<evict_select_kernel<false>>(bytes(1))) != MPFA_OK) return rc;
+    if ((rc = allow_smem<evict_select_kernel<false>>(SEL_CACHE * sizeof(uint32_t))) != MPFA_OK) return rc;
     MPFA_CUDA_OK(launch(evict_select_kernel<false>, grid(1), dim3(SEL_THREADS), bytes(1), s, p, 1));
   }
   const int pages = (keep + PAGE - 1) / PAGE;
