@@ -864,7 +864,7 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
                   const size_t slots = (size_t)p.max_pages * PAGE;
                   float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + k_part + (w.nblk - 1 - t) * TILE + r;
 #pragma unroll
-                  for (int g = 0; g < G; ++g) x[g * slots] = __uint_as_float(sr[u][g]);
+                  for (int g = 0; g < G; ++g) x[g * slots] = fmaxf(__uint_as_float(sr[u][g]), -INFINITY);   // a NaN receives nothing
                 }
               }
 #pragma unroll
@@ -1134,7 +1134,8 @@ __global__ void __launch_bounds__(W_THREADS) decode_weights_kernel(const __grid_
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const float c = -__fmul_rn(ml[g].x, lam), inv = ml[g].y > 0.0f ? __frcp_rn(ml[g].y) : 0.0f;
+      if (!(ml[g].y > 0.0f)) continue;   // no softmax, and no output either: exponents would be NaN, which no factor takes out
+      const float c = -__fmul_rn(ml[g].x, lam), inv = __frcp_rn(ml[g].y);
       w.x = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].x, lam, c)), inv, w.x);
       w.y = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].y, lam, c)), inv, w.y);
       w.z = __fmaf_rn(ex2_approx(__fmaf_rn(x[g].z, lam, c)), inv, w.z);

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import bounded_plain as plain
+import test_gpu_bounded as bounded
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,79 @@ def test_host_threads_evict_from_tables_of_different_widths(pages):
     for kv, table, lens, w, keep, sinks, recent, _, kept, new_lens, _, status, _ in jobs:
         assert int(status) == 0 and new_lens.tolist() == [keep]
         assert np.array_equal(kept[0, 0].cpu().numpy(), plain.evicted(w[0, 0].cpu().numpy(), w.shape[2], keep, sinks, recent))
+
+
+# ------------------------------------------------------------------------------------------------------------------ weights
+def sums_of(st, table, old):
+    """One step that adds to a copy of `old`: (sums, out, out_f32, status)."""
+    B = binding()
+    weights, out, o32 = old.clone(), torch.empty_like(st.out), torch.empty_like(st.out_f32)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mpfa_decode_weights(st.q4, st.kv, table, st.seq_lens, st.stats, st.v_scale, st.softmax_scale, weights, out, o32,
+                          B.decode_weights_workspace(st.q4.B, st.kv.H_q, st.kv.H_kv, table.shape[1]), status)
+    torch.cuda.synchronize()
+    return weights, out, o32, int(status)
+
+
+def random_sums(st, seed):
+    shape = st.q4.B, st.kv.H_kv, st.page_table.shape[1] * 64
+    return torch.rand(*shape, generator=torch.Generator().manual_seed(seed)).cuda()
+
+
+def close_sums(got, old, want, what):
+    """As for whole caches: each weight off by NEAR twice (exponent, l), and one rounding of the sum."""
+    old, got = old.cpu().numpy().astype(np.float64), got.cpu().numpy()
+    bounded.close(got, old + want, 2 * plain.NEAR * want + 2.0 ** -24 * (old + want) * (1 + 2.0 ** -20), what)
+
+
+def set_delta(kv, page, h, t, value):
+    kv.delta[page, h, ((t // 8) ^ (h % (kv.H_q // kv.H_kv))) * 8 + t % 8] = value
+
+
+@pytest.mark.parametrize("H_q,H_kv", [(4, 4), (4, 2), (8, 1)])
+@pytest.mark.parametrize("value", [-float("inf"), float("nan"), float("inf")])
+@pytest.mark.parametrize("lens", [[300, 64], [2600, 1500], [5000, 4097]])   # one partition; a few; many
+def test_heads_without_a_softmax_add_nothing(H_q, H_kv, value, lens):
+    """All logits of a kv head's q heads -infinity, NaN or +infinity: no output, and no trace in the sums."""
+    from paper_2609_33135_b200 import decode_cache
+    st, G = bounded.state(1520 + H_q, lens, H_q, H_kv), H_q // H_kv
+    bad = H_kv - 1
+    for h in range(bad * G, bad * G + G):
+        for i in range(-(-lens[0] // 64)):
+            st.kv.delta[int(st.page_table[0, i]), h] = value
+    old = random_sums(st, 2)
+    weights, out, o32, status = sums_of(st, st.page_table, old)
+    decode_cache.decode_step(st)
+    torch.cuda.synchronize()
+    assert status == 0 and torch.equal(out, st.out) and torch.equal(o32, st.out_f32)
+    assert not o32[0, bad * G:].any() and torch.equal(weights[0, bad], old[0, bad])
+    for b, L in enumerate(lens):
+        want = bounded.plain_weights(st, b)
+        heads = [hk for hk in range(H_kv) if b or hk != bad]
+        if heads:
+            close_sums(weights[b, heads, :L], old[b, heads, :L], want[heads], b)
+
+
+def test_logits_that_are_no_numbers_leave_the_sums_numbers():
+    """One NaN scale: the heads that see the key have no softmax.  A partition of nothing else is left out, and its keys receive nothing."""
+    lens, H_q, H_kv = [300, 2600], 8, 4
+    st = bounded.state(1530, lens, H_q, H_kv)
+    st.kv.k_sf[int(st.page_table[0, 0]), 0, 5 * 8:5 * 8 + 8] = 0x7F
+    for i in range(16, 32):
+        st.kv.k_sf[int(st.page_table[1, i]), 2] = 0x7F
+    old = random_sums(st, 3)
+    weights, out, o32, status = sums_of(st, st.page_table, old)
+    assert status == 0 and bool(torch.isfinite(weights).all())
+    assert not o32[0, :2].any() and torch.equal(weights[0, 0], old[0, 0])
+    assert torch.equal(weights[1, 2, 1024:2048], old[1, 2, 1024:2048])
+    lam, q = plain.lam_of(st.stats, 1, st.softmax_scale), plain.tile_rows(st.q4)
+    K, V, D = plain.cached(st.kv, st.page_table[1].cpu().numpy(), 2600)
+    there = np.r_[0:1024, 2048:2600]
+    want = np.zeros(len(there))
+    for h in (4, 5):
+        S = q[1, h, 0] @ K[2, there].T + D[h, there]
+        P = np.exp2(lam * (S - S.max()))
+        want += P / P.sum()
+    close_sums(weights[1, 2, there], old[1, 2, there], want, "beside the partition")
+    for b, heads in ((0, [1, 2, 3]), (1, [0, 1, 3])):
+        close_sums(weights[b, heads, :lens[b]], old[b, heads, :lens[b]], bounded.plain_weights(st, b)[heads], b)
