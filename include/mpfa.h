@@ -363,7 +363,8 @@ mpfa_status mpfa_decode_window(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *
  * the softmax weights before P is rounded, in FP32.  weights is [B, H_kv, weights_stride] FP32 with weights_stride >= 64 *
  * max_pages_per_req (else MPFA_ERR_INVALID_ARG); entries from seq_lens[b] on are left as they are.  A caller starts a token's sum at 0.
  * A head whose l is not a positive number (all of its logits -infinity or NaN, say), whose output is zero, adds nothing, and a key whose
- * logit is NaN receives nothing.
+ * logit is NaN receives nothing.  Keys on a page outside [0, num_pages) (MPFA_DEV_BAD_PAGE) are in no softmax here and receive nothing: the
+ * sums outlive the call.
  * The output is mpfa_decode's.  seq_lens[b] above 64 * max_pages_per_req is treated as that bound.  The workspace also holds the logits:
  * mpfa_decode_weights_workspace_bytes(); calls that overlap on the GPU need separate ones, and separate sums. */
 mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv *h_kv, const int32_t *page_table,

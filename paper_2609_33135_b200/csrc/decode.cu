@@ -785,12 +785,20 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
       const float lam = w.b < D_MAXREQ ? lam_tab[w.b]
                                        : __fmul_rn(__fmul_rn(__fmul_rn(p.softmax_scale, 1.4426950408889634f), p.q_gscale[w.b]), p.k_gscale[w.b]);
       const int k_part = w.sp * DECODE_SPLIT;
+      // WEIGHTS: which blocks have this warp's half on a page of the pool.  The sums outlive the call, so keys on another one, of which the ring
+      // holds what was there before, are left out of the softmax; lane l looks at block l, while the scores are not there yet.
+      int page = 0;
+      if (MODE == WEIGHTS && lane < w.nblk) {
+        const int pg = (w.sp * MAXBLK + lane) * (TILE / PAGE) + (quad >> 1);
+        page = pg < p.max_pages ? p.page_table[(size_t)w.b * p.max_pages + pg] : -1;
+      }
       // ---- all scores of the item at once.  They are read from tensor memory twice, once for the maxima and once for the
       // exponentials: held in registers in between, MAXBLK x G of them and as many maxima went to local memory for groups
       // of five heads and more (24 us per item instead of 6).
       ok = cx.wait_warp(B_S_FULL + par, ph);
       if (!ok) break;
       tc_fence_after();
+      const uint32_t there = MODE == WEIGHTS ? __ballot_sync(0xffffffffu, page >= 0 && page < p.num_pages) : ~0u;
       // block maxima of this warp's keys, CH blocks at a time
 #pragma unroll 1
       for (int t0 = grp; t0 < w.nblk; t0 += 2 * CH) {
@@ -803,7 +811,8 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
         for (int u = 0; u < CH; ++u) {
           const int t = t0 + 2 * u;
           if (t < w.nblk) {
-            const bool valid = p.visible<MODE>(k_part + (w.nblk - 1 - t) * TILE + r, w.L);
+            const int blk = w.nblk - 1 - t;
+            const bool valid = p.visible<MODE>(k_part + blk * TILE + r, w.L) && (MODE != WEIGHTS || (there >> blk & 1u));
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               const float wm = warp_max(valid ? __uint_as_float(sr[u][g]) : -INFINITY);
@@ -857,14 +866,15 @@ __global__ void __launch_bounds__(G <= 4 ? 896 : D_THREADS, 1) decode_split_kern
           for (int u = 0; u < CH; ++u) {
             const int t = v * TPV + t0 + 2 * u;
             if (t < w.nblk) {
-              const bool valid = p.visible<MODE>(k_part + (w.nblk - 1 - t) * TILE + r, w.L);
+              const int blk = w.nblk - 1 - t, key = k_part + blk * TILE + r;
+              const bool valid = p.visible<MODE>(key, w.L) && (MODE != WEIGHTS || (there >> blk & 1u));
               float pq[G + 1];
               if constexpr (MODE == WEIGHTS) {
-                if (valid) {
+                if (key < w.L) {
                   const size_t slots = (size_t)p.max_pages * PAGE;
-                  float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + k_part + (w.nblk - 1 - t) * TILE + r;
+                  float *const x = p.logits + ((size_t)w.b * p.H_q + (size_t)w.hk * G) * slots + key;
 #pragma unroll
-                  for (int g = 0; g < G; ++g) x[g * slots] = fmaxf(__uint_as_float(sr[u][g]), -INFINITY);   // a NaN receives nothing
+                  for (int g = 0; g < G; ++g) x[g * slots] = valid ? fmaxf(__uint_as_float(sr[u][g]), -INFINITY) : -INFINITY;   // a NaN receives nothing
                 }
               }
 #pragma unroll

@@ -133,3 +133,38 @@ def test_logits_that_are_no_numbers_leave_the_sums_numbers():
     close_sums(weights[1, 2, there], old[1, 2, there], want, "beside the partition")
     for b, heads in ((0, [1, 2, 3]), (1, [0, 1, 3])):
         close_sums(weights[b, heads, :lens[b]], old[b, heads, :lens[b]], bounded.plain_weights(st, b)[heads], b)
+
+
+@pytest.mark.parametrize("H_q,H_kv", [(4, 4), (8, 2), (10, 2), (16, 2)])
+def test_keys_on_missing_pages_receive_no_weight(H_q, H_kv):
+    """They are in no softmax either: the others' weights, and the output, are those of the keys that are there."""
+    B = binding()
+    lens = [2600, 700, 64]
+    st, G = bounded.state(1500 + H_q, lens, H_q, H_kv, v_scale=0.5), H_q // H_kv
+    old = random_sums(st, 1)
+    clean, clean_out, _, status = sums_of(st, st.page_table, old)
+    assert status == 0
+    table = st.page_table.clone()
+    gone = {0: [3] + list(range(16, 32)) + [40], 1: [], 2: [0]}   # a page, a whole partition and the last page; none; all
+    for b, pages in gone.items():
+        for i in pages:
+            table[b, i] = (-1, st.kv.num_pages, 2 ** 31 - 1)[i % 3]
+    weights, out, o32, status = sums_of(st, table, old)
+    assert status == B.MPFA_DEV_BAD_PAGE
+    assert torch.equal(weights[1], clean[1]) and torch.equal(out[1], clean_out[1])
+    assert torch.equal(weights[2], old[2]) and not o32[2].any()
+    L = lens[0]
+    there = np.ones(L, bool)
+    for i in gone[0]:
+        there[i * 64:i * 64 + 64] = False
+    K, V, D = plain.cached(st.kv, st.page_table[0].cpu().numpy(), L)
+    lam, q = plain.lam_of(st.stats, 0, st.softmax_scale), plain.tile_rows(st.q4)
+    want = np.zeros((H_kv, L))
+    for h in range(H_q):
+        o, room, top, l = plain.attend(q[0, h], K[h // G], V[h // G], D[h], there[None], lam, 0.5, 8)
+        bounded.close(o32[0, h].cpu().numpy(), o[0], room[0], h)
+        S = np.where(there, q[0, h, 0] @ K[h // G].T + D[h], -np.inf)
+        want[h // G] += np.exp2(lam * (S - top[0])) / l[0]
+    close_sums(weights[0, :, :L], old[0, :, :L], want, "present")
+    absent = torch.from_numpy(~there).cuda()
+    assert torch.equal(weights[0, :, :L][:, absent], old[0, :, :L][:, absent]) and torch.equal(weights[0, :, L:], old[0, :, L:])
