@@ -75,7 +75,7 @@ def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, we
 def attention_sums(s: DecodeState) -> torch.Tensor:
     """Zeroed sums for decode_step(weights=...), and a workspace of `s` that is large enough for it."""
     s.workspace = B_.decode_weights_workspace(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1], s.page_table.device)
-    return torch.zeros(s.w.B, s.w.H_kv, s.page_table.shape[1] * B_.PAGE, device=s.page_table.device)
+    return torch.zeros(s.w.B, s.w.H_kv, s.page_table.shape[1] * B_.PAGE, dtype=torch.float32, device=s.page_table.device)
 
 
 def evict(s: DecodeState, weights: torch.Tensor, keep: int, sinks: int, recent: int, new_pages: torch.Tensor):
@@ -85,7 +85,7 @@ def evict(s: DecodeState, weights: torch.Tensor, keep: int, sinks: int, recent: 
     dev = s.page_table.device
     kept = torch.empty(s.w.B, s.w.H_kv, keep, dtype=torch.int32, device=dev)
     new_lens = torch.empty_like(s.seq_lens)
-    new_weights = torch.empty(s.w.B, s.w.H_kv, new_pages.shape[1] * B_.PAGE, device=dev)
+    new_weights = torch.empty(s.w.B, s.w.H_kv, new_pages.shape[1] * B_.PAGE, dtype=torch.float32, device=dev)
     B_.mpfa_evict_paged(s.kv, s.page_table, s.seq_lens, weights, keep, sinks, recent, new_pages, kept, new_lens, new_weights, s.status)
     s.page_table, s.seq_lens = new_pages, new_lens
     return kept, new_weights

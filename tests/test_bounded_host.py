@@ -1,0 +1,40 @@
+"""CPU: what the cache module keeps and replaces for requests whose cache is bounded."""
+import pytest
+import torch
+
+from paper_2609_33135_b200 import workloads as wl
+
+
+@pytest.fixture
+def module(monkeypatch):
+    """The cache module with the library's calls noted instead of made."""
+    from paper_2609_33135_b200 import binding, build, decode_cache
+    build.build()
+    calls = []
+    for name in ("mpfa_decode", "mpfa_decode_window", "mpfa_decode_weights", "mpfa_evict_paged"):
+        monkeypatch.setattr(binding, name, lambda *a, name=name: calls.append((name, a)))
+    decode_cache.calls = calls
+    yield decode_cache
+    del decode_cache.calls
+
+
+def state(module, pages):
+    from paper_2609_33135_b200 import binding as B
+    w = wl.decode_workload("host", 3, 2, 8, 2, 1, pages * 64, seq_lens=[pages * 64, 5])
+    table = torch.zeros(2, pages, dtype=torch.int32)
+    return module.DecodeState(w, B.PagedKV.empty(4, 8, 2, device="cpu"), B.Stats.empty(2, 8, 2, "cpu"), None, table, w.seq_lens.clone(),
+                              B.decode_workspace(2, 8, 2, pages, "cpu"), torch.empty(2, 8, 128, dtype=torch.bfloat16), None,
+                              torch.zeros(1, dtype=torch.int32), 1.0, 0.1)
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_sums_are_fp32_whatever_torchs_default_type(module, default):
+    """Programs that build their model in BF16 by setting the default type."""
+    st = state(module, 4)
+    torch.set_default_dtype(default)
+    try:
+        sums = module.attention_sums(st)
+        _, new_sums = module.evict(st, sums, 100, 4, 10, torch.ones(2, 2, dtype=torch.int32))
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert sums.dtype == torch.float32 and new_sums.dtype == torch.float32
