@@ -27,6 +27,7 @@ class DecodeState:
     status: torch.Tensor
     v_scale: float
     softmax_scale: float
+    sums_workspace: Optional[torch.Tensor] = None   # of steps that sum weights, once there are sums
 
 
 def build_cache(w: DecodeWorkload, device="cuda", smooth: bool = True, v_scale: float = 1.0,
@@ -65,7 +66,7 @@ def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, we
                               s.workspace, s.status)
     elif weights is not None:
         B_.mpfa_decode_weights(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, s.softmax_scale, weights, s.out, s.out_f32,
-                               s.workspace, s.status)
+                               s.workspace if s.sums_workspace is None else s.sums_workspace, s.status)
     else:
         B_.mpfa_decode(s.q4, s.kv, s.page_table, s.seq_lens, s.stats, s.v_scale, s.softmax_scale, s.out, s.out_f32,
                        s.workspace, s.status)
@@ -73,8 +74,10 @@ def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, we
 
 
 def attention_sums(s: DecodeState) -> torch.Tensor:
-    """Zeroed sums for decode_step(weights=...), and a workspace of `s` that is large enough for it."""
-    s.workspace = B_.decode_weights_workspace(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1], s.page_table.device)
+    """Zeroed sums for decode_step(weights=...), and a workspace for those steps.  The others' stays, since a captured step holds its address."""
+    n = B_.lib().mpfa_decode_weights_workspace_bytes(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1])
+    if s.sums_workspace is None or s.sums_workspace.numel() < n:
+        s.sums_workspace = B_.decode_weights_workspace(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1], s.page_table.device)
     return torch.zeros(s.w.B, s.w.H_kv, s.page_table.shape[1] * B_.PAGE, dtype=torch.float32, device=s.page_table.device)
 
 

@@ -38,3 +38,18 @@ def test_sums_are_fp32_whatever_torchs_default_type(module, default):
     finally:
         torch.set_default_dtype(torch.float32)
     assert sums.dtype == torch.float32 and new_sums.dtype == torch.float32
+
+
+def test_sums_have_a_workspace_of_their_own(module):
+    st = state(module, 20)
+    plain = st.workspace
+    sums = module.attention_sums(st)
+    assert st.workspace is plain and sums.shape == (2, 2, 1280)
+    first = st.sums_workspace
+    module.attention_sums(st)
+    assert st.sums_workspace is first   # large enough still
+    module.decode_step(st)
+    module.decode_step(st, window=9)
+    module.decode_step(st, weights=sums)
+    used = {name: a[-2] for name, a in module.calls}   # the workspace stands before the status
+    assert used["mpfa_decode"] is plain and used["mpfa_decode_window"] is plain and used["mpfa_decode_weights"] is first

@@ -168,3 +168,24 @@ def test_keys_on_missing_pages_receive_no_weight(H_q, H_kv):
     close_sums(weights[0, :, :L], old[0, :, :L], want, "present")
     absent = torch.from_numpy(~there).cuda()
     assert torch.equal(weights[0, :, :L][:, absent], old[0, :, :L][:, absent]) and torch.equal(weights[0, :, L:], old[0, :, L:])
+
+
+# ------------------------------------------------------------------------------------------------------------------ the cache module
+def test_sums_leave_the_workspace_of_captured_steps_alone():
+    """A graph of a plain step, then sums for the same requests, then the graph again while other tensors take what was given up."""
+    from paper_2609_33135_b200 import decode_cache
+    st = bounded.state(1570, [2600, 1500], 8, 2)
+    decode_cache.decode_step(st)
+    want = st.out.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        decode_cache.decode_step(st)
+    n = st.workspace.numel()
+    sums = decode_cache.attention_sums(st)
+    filled = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    st.out.zero_()
+    graph.replay()
+    decode_cache.decode_step(st, weights=sums)
+    torch.cuda.synchronize()
+    assert torch.equal(st.out, want) and all(bool((f == 7).all()) for f in filled)
