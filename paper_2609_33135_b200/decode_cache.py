@@ -73,11 +73,19 @@ def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, we
     return s.out
 
 
+def _fit_workspaces(s: DecodeState, sums: bool = False) -> None:
+    """Larger ones where the page table has outgrown those that are there; with `sums` one for steps that sum weights too."""
+    shape, dev = (s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1]), s.page_table.device
+    if s.workspace.numel() < B_.lib().mpfa_decode_workspace_bytes(*shape):
+        s.workspace = B_.decode_workspace(*shape, dev)
+    have = -1 if s.sums_workspace is None else s.sums_workspace.numel()
+    if (sums or have >= 0) and have < B_.lib().mpfa_decode_weights_workspace_bytes(*shape):
+        s.sums_workspace = B_.decode_weights_workspace(*shape, dev)
+
+
 def attention_sums(s: DecodeState) -> torch.Tensor:
     """Zeroed sums for decode_step(weights=...), and a workspace for those steps.  The others' stays, since a captured step holds its address."""
-    n = B_.lib().mpfa_decode_weights_workspace_bytes(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1])
-    if s.sums_workspace is None or s.sums_workspace.numel() < n:
-        s.sums_workspace = B_.decode_weights_workspace(s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1], s.page_table.device)
+    _fit_workspaces(s, sums=True)
     return torch.zeros(s.w.B, s.w.H_kv, s.page_table.shape[1] * B_.PAGE, dtype=torch.float32, device=s.page_table.device)
 
 
@@ -91,4 +99,5 @@ def evict(s: DecodeState, weights: torch.Tensor, keep: int, sinks: int, recent: 
     new_weights = torch.empty(s.w.B, s.w.H_kv, new_pages.shape[1] * B_.PAGE, dtype=torch.float32, device=dev)
     B_.mpfa_evict_paged(s.kv, s.page_table, s.seq_lens, weights, keep, sinks, recent, new_pages, kept, new_lens, new_weights, s.status)
     s.page_table, s.seq_lens = new_pages, new_lens
+    _fit_workspaces(s)
     return kept, new_weights

@@ -53,3 +53,19 @@ def test_sums_have_a_workspace_of_their_own(module):
     module.decode_step(st, weights=sums)
     used = {name: a[-2] for name, a in module.calls}   # the workspace stands before the status
     assert used["mpfa_decode"] is plain and used["mpfa_decode_window"] is plain and used["mpfa_decode_weights"] is first
+
+
+@pytest.mark.parametrize("pages", [2, 20, 21, 500])
+def test_workspaces_follow_the_table_after_an_eviction(module, pages):
+    from paper_2609_33135_b200 import binding as B
+    st = state(module, 20)
+    sums = module.attention_sums(st)
+    was = st.workspace, st.sums_workspace
+    new_pages = torch.ones(2, pages, dtype=torch.int32)
+    kept, new_sums = module.evict(st, sums, 100, 4, 10, new_pages)
+    assert st.page_table is new_pages and kept.shape == (2, 2, 100) and new_sums.shape == (2, 2, pages * 64)
+    L = B.lib()
+    assert st.workspace.numel() >= L.mpfa_decode_workspace_bytes(2, 8, 2, pages)
+    assert st.sums_workspace.numel() >= L.mpfa_decode_weights_workspace_bytes(2, 8, 2, pages)
+    if pages <= 20:
+        assert st.workspace is was[0] and st.sums_workspace is was[1]

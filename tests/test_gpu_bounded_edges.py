@@ -171,6 +171,37 @@ def test_keys_on_missing_pages_receive_no_weight(H_q, H_kv):
 
 
 # ------------------------------------------------------------------------------------------------------------------ the cache module
+def with_spare_pages(st, spare):
+    """The same requests in a pool with `spare` more pages; their ids."""
+    B = binding()
+    n, big = st.kv.num_pages, B.PagedKV.empty(st.kv.num_pages + spare, st.kv.H_q, st.kv.H_kv)
+    for new, old in ((big.k_codes, st.kv.k_codes), (big.k_sf, st.kv.k_sf), (big.v_fp8, st.kv.v_fp8), (big.delta, st.kv.delta)):
+        new[:n] = old
+    st.kv = big
+    return torch.arange(n, n + spare, dtype=torch.int32, device="cuda")
+
+
+def test_a_cache_that_is_cut_back_goes_on_in_a_wider_table():
+    """Room for the tokens that follow: more partitions and more logits than the table before had."""
+    from paper_2609_33135_b200 import decode_cache
+    outs, grown = [], []
+    for width in (5, 80):
+        st = bounded.state(1540, [900, 300], 8, 2)
+        sums = decode_cache.attention_sums(st)
+        decode_cache.decode_step(st, weights=sums)
+        new_pages = with_spare_pages(st, 2 * width).view(2, width)
+        kept, new_sums = decode_cache.evict(st, sums, 300, 4, 100, new_pages)
+        assert new_sums.shape == (2, 2, width * 64) and not new_sums[:, :, 300:].any()
+        plain_step = decode_cache.decode_step(st).clone()
+        assert torch.equal(decode_cache.decode_step(st, window=1 << 20), plain_step)
+        assert torch.equal(decode_cache.decode_step(st, weights=new_sums), plain_step)
+        again = decode_cache.attention_sums(st)
+        decode_cache.decode_step(st, weights=again)
+        torch.cuda.synchronize()
+        assert int(st.status) == 0
+        outs.append(plain_step)
+        grown.append(new_sums[:, :, :320])
+    assert torch.equal(*outs) and torch.equal(*grown)
 def test_sums_leave_the_workspace_of_captured_steps_alone():
     """A graph of a plain step, then sums for the same requests, then the graph again while other tensors take what was given up."""
     from paper_2609_33135_b200 import decode_cache
