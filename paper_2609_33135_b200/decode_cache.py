@@ -4,8 +4,8 @@ query statistics, quantizes the decode-step query and issues mpfa_decode.  All a
 in the library's kernels; this module only sequences calls and owns the device buffers."""
 from __future__ import annotations
 
-from dataclasses import dataclass
-from typing import Optional
+from dataclasses import dataclass, field
+from typing import List, Optional
 
 import torch
 
@@ -28,6 +28,7 @@ class DecodeState:
     v_scale: float
     softmax_scale: float
     sums_workspace: Optional[torch.Tensor] = None   # of steps that sum weights, once there are sums
+    captured: List[torch.Tensor] = field(default_factory=list)   # given up during a capture: a replay reads them
 
 
 def build_cache(w: DecodeWorkload, device="cuda", smooth: bool = True, v_scale: float = 1.0,
@@ -73,13 +74,27 @@ def decode_step(s: DecodeState, window: Optional[int] = None, sinks: int = 0, we
     return s.out
 
 
+def _give_up(s: DecodeState, t: torch.Tensor) -> None:
+    """Before `s` lets go of a tensor that calls of the current stream may still have to read, which the allocator knows only of the stream that
+    it was made on.  A graph that is being captured reads it whenever it is replayed."""
+    if not t.is_cuda:
+        return
+    if torch.cuda.is_current_stream_capturing():
+        s.captured.append(t)
+    else:
+        t.record_stream(torch.cuda.current_stream(t.device))
+
+
 def _fit_workspaces(s: DecodeState, sums: bool = False) -> None:
     """Larger ones where the page table has outgrown those that are there; with `sums` one for steps that sum weights too."""
     shape, dev = (s.w.B, s.w.H_q, s.w.H_kv, s.page_table.shape[1]), s.page_table.device
     if s.workspace.numel() < B_.lib().mpfa_decode_workspace_bytes(*shape):
+        _give_up(s, s.workspace)
         s.workspace = B_.decode_workspace(*shape, dev)
     have = -1 if s.sums_workspace is None else s.sums_workspace.numel()
     if (sums or have >= 0) and have < B_.lib().mpfa_decode_weights_workspace_bytes(*shape):
+        if have >= 0:
+            _give_up(s, s.sums_workspace)
         s.sums_workspace = B_.decode_weights_workspace(*shape, dev)
 
 
@@ -92,12 +107,16 @@ def attention_sums(s: DecodeState) -> torch.Tensor:
 def evict(s: DecodeState, weights: torch.Tensor, keep: int, sinks: int, recent: int, new_pages: torch.Tensor):
     """Cuts every request's cache back to `keep` tokens a kv head, by `weights`, into the pages of new_pages [B, >= ceil(keep / 64)] (int32; of
     the same pools, in no request's table); from then on `s` has those pages and lengths, and the old pages are the caller's again.
-    Returns (the kept tokens' former slots, their sums for further steps: a row is as wide as the new table)."""
+    Returns (the kept tokens' former slots, their sums for further steps: a row is as wide as the new table).
+    A graph captured of steps before the eviction has the old table, lengths and workspaces; it is not replayed after it, nor is one with an
+    eviction in it once the state is gone."""
     dev = s.page_table.device
     kept = torch.empty(s.w.B, s.w.H_kv, keep, dtype=torch.int32, device=dev)
     new_lens = torch.empty_like(s.seq_lens)
     new_weights = torch.empty(s.w.B, s.w.H_kv, new_pages.shape[1] * B_.PAGE, dtype=torch.float32, device=dev)
     B_.mpfa_evict_paged(s.kv, s.page_table, s.seq_lens, weights, keep, sinks, recent, new_pages, kept, new_lens, new_weights, s.status)
+    _give_up(s, s.page_table)
+    _give_up(s, s.seq_lens)
     s.page_table, s.seq_lens = new_pages, new_lens
     _fit_workspaces(s)
     return kept, new_weights

@@ -202,6 +202,59 @@ def test_a_cache_that_is_cut_back_goes_on_in_a_wider_table():
         outs.append(plain_step)
         grown.append(new_sums[:, :, :320])
     assert torch.equal(*outs) and torch.equal(*grown)
+
+@pytest.mark.parametrize("width", [5, 80])   # narrower than the table before, wider
+def test_eviction_on_another_stream_than_the_caches(width):
+    """What the state gives up is read by calls that have not run yet: other tensors must not get its memory before."""
+    from paper_2609_33135_b200 import decode_cache
+    sts = [bounded.state(1550, [900, 300], 8, 2) for _ in range(2)]
+    kept, outs = [], []
+    for k, st in enumerate(sts):
+        sums = decode_cache.attention_sums(st)
+        decode_cache.decode_step(st, weights=sums)
+        new_pages = with_spare_pages(st, 2 * width).view(2, width)
+        shapes = [(t.shape, t.dtype) for t in (st.page_table, st.seq_lens, st.workspace)]
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            if k:
+                torch.cuda._sleep(200_000_000)   # a tenth of a second, so that everything below is asked for before it runs
+            kept.append(decode_cache.evict(st, sums, 300, 4, 100, new_pages)[0])
+        filled = [torch.full(shape, 1, dtype=dtype, device="cuda") for shape, dtype in shapes for _ in range(64)]
+        torch.cuda.synchronize()
+        outs.append(decode_cache.decode_step(st).clone())
+        assert int(st.status) == 0 and len(filled) == 192
+    assert torch.equal(*kept) and torch.equal(*outs)
+
+
+@pytest.mark.parametrize("width", [5, 80])
+def test_a_captured_eviction_keeps_what_it_reads(width):
+    """Steps before and after an eviction in one graph, replayed after other tensors have taken all memory that was free."""
+    from paper_2609_33135_b200 import decode_cache
+
+    def serve(st, sums, new_pages):
+        first = decode_cache.decode_step(st, weights=sums).clone()
+        kept, new_sums = decode_cache.evict(st, sums, 300, 4, 100, new_pages)
+        return first, kept, new_sums, decode_cache.decode_step(st, weights=new_sums).clone()
+
+    def fresh():
+        st = bounded.state(1560, [900, 300], 8, 2)
+        return st, decode_cache.attention_sums(st), with_spare_pages(st, 2 * width).view(2, width)
+
+    eager = serve(*fresh())
+    torch.cuda.synchronize()
+    st, sums, new_pages = fresh()
+    shapes = [(t.shape, t.dtype) for t in (st.page_table, st.seq_lens, st.workspace)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = serve(st, sums, new_pages)
+    filled = [torch.full(shape, 1, dtype=dtype, device="cuda") for shape, dtype in shapes for _ in range(64)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(st.status) == 0 and len(filled) == 192
+    for a, b in zip(eager, captured):
+        assert torch.equal(a, b)
 def test_sums_leave_the_workspace_of_captured_steps_alone():
     """A graph of a plain step, then sums for the same requests, then the graph again while other tensors take what was given up."""
     from paper_2609_33135_b200 import decode_cache
