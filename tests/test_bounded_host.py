@@ -1,8 +1,14 @@
-"""CPU: what the cache module keeps and replaces for requests whose cache is bounded."""
+"""CPU: what the cache module keeps and replaces for requests whose cache is bounded, and the callables of those calls: what they convert and
+refuse."""
+import os
+import re
+
 import pytest
 import torch
 
 from paper_2609_33135_b200 import workloads as wl
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture
@@ -69,3 +75,33 @@ def test_workspaces_follow_the_table_after_an_eviction(module, pages):
     assert st.sums_workspace.numel() >= L.mpfa_decode_weights_workspace_bytes(2, 8, 2, pages)
     if pages <= 20:
         assert st.workspace is was[0] and st.sums_workspace is was[1]
+
+
+def entries():
+    """name -> kinds of all callables."""
+    text = open(os.path.join(ROOT, "paper_2609_33135_b200", "csrc", "calls.c")).read()
+    return dict(re.findall(r'^(?:ENTRY|BOUNDED)\((\w+), "(\w+)",', text, flags=re.M))
+
+
+def test_every_callable_is_found():
+    assert len(entries()) == 12
+
+
+@pytest.mark.parametrize("name", sorted(entries()))
+def test_conversions_and_what_is_refused(name):
+    from paper_2609_33135_b200 import binding, build
+    build.build()
+    kinds, call = entries()[name], getattr(binding.lib(), "packed_" + name)
+    null = [{"p": None, "i": 1, "f": 1.0, "z": 0}[c] for c in kinds]
+    assert call(*null) == -1 and call(*[0 if c == "p" else x for c, x in zip(kinds, null)]) == -1   # None and 0 are null pointers
+    for args in (null[:-1], null + [None], []):
+        with pytest.raises(TypeError, match="arguments"):
+            call(*args)
+    bad = {"p": ("text", 1.5, bytearray(8)), "i": (None, 1.5, b"1"), "f": (None, "1"), "z": (None, 1.5)}
+    for k, c in enumerate(kinds):
+        for x in bad[c]:
+            with pytest.raises(TypeError):
+                call(*null[:k], x, *null[k + 1:])
+        for x in {"i": (1 << 31, -(1 << 31) - 1, 1 << 70), "z": (-1, 1 << 64)}.get(c, ()):
+            with pytest.raises(OverflowError):
+                call(*null[:k], x, *null[k + 1:])

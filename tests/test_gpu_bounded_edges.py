@@ -8,6 +8,7 @@ import torch
 
 import bounded_plain as plain
 import test_gpu_bounded as bounded
+from paper_2609_33135_b200 import workloads as wl
 
 pytestmark = pytest.mark.gpu
 
@@ -273,3 +274,172 @@ def test_sums_leave_the_workspace_of_captured_steps_alone():
     decode_cache.decode_step(st, weights=sums)
     torch.cuda.synchronize()
     assert torch.equal(st.out, want) and all(bool((f == 7).all()) for f in filled)
+
+
+# ------------------------------------------------------------------------------------------------------------------ hidden values
+def nan_at(kv, page, t):
+    """K scales and Delta_S of one cached token."""
+    kv.k_sf[page, :, t * 8:t * 8 + 8] = 0x7F
+    for h in range(kv.H_q):
+        set_delta(kv, page, h, t, float("nan"))
+
+
+@pytest.mark.parametrize("lens,q_lens,window,sinks", [
+    ([900, 333], None, 100, 5),
+    ([1000, 200], [70, 130], 300, 70),
+    ([6000], None, 4500, 90),        # accumulated in runs
+    ([129, 1], [1, 1], 1, 0),
+])
+def test_a_chunk_does_not_see_hidden_values_of_pages_that_stay(lens, q_lens, window, sinks):
+    """Tokens out of every query's view hold NaN in K and Delta_S; so do those behind the context in its last page."""
+    B = binding()
+    N_q, nb, H_q, H_kv = 130, len(lens), 8, 2
+    st = bounded.state(1580, lens, H_q, H_kv)
+    q4 = B.Fp4Tensor.empty(nb, H_q, N_q)
+    B.mpfa_quantize_qk(torch.randn(nb, N_q, H_q, 128, generator=torch.Generator().manual_seed(6)).bfloat16().cuda(), None,
+                       B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    n = [min(N_q, L) for L in lens] if q_lens is None else q_lens
+    n_t = torch.tensor(n, dtype=torch.int32, device="cuda")
+
+    def chunk():
+        out, o32 = torch.empty(nb, N_q, H_q, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(nb, N_q, H_q, 128, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.mpfa_prefill_paged_window(q4, st.kv, st.page_table, st.seq_lens, st.stats, 1.0, window, sinks, st.softmax_scale, out, o32, status, n_t)
+        assert int(status) == 0
+        return o32
+
+    clean, hidden = chunk(), 0
+    for b, L in enumerate(lens):
+        low = max(L - n[b] - window + 1, 0)
+        for i in range(-(-L // 64)):
+            for t in range(64):
+                if sinks <= i * 64 + t < low or i * 64 + t >= L:
+                    nan_at(st.kv, int(st.page_table[b, i]), t)
+                    hidden += 1
+    assert hidden
+    assert torch.equal(chunk(), clean) and bool(clean.any())
+
+
+@pytest.mark.parametrize("N_q,N_kv,window,sinks", [(130, 900, 100, 5), (200, 1000, 300, 70), (130, 6000, 4500, 90), (1, 333, 1, 0)])
+def test_a_prompt_does_not_see_hidden_values(N_q, N_kv, window, sinks):
+    """The same on contiguous operands with fewer queries than keys."""
+    B = binding()
+    w = wl.prefill_workload("hidden", 1590, 2, N_kv, 4, 2, True)
+    s1 = B.stage1(w.q[:, :N_q].contiguous().cuda(), w.k.cuda(), w.v.cuda())
+
+    def prompt():
+        out, o32 = torch.empty(2, N_q, 4, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(2, N_q, 4, 128, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.mpfa_prefill_window(s1.q, s1.k, s1.v_fp8, s1.delta, s1.stats, 1.0, window, sinks, w.softmax_scale, out, o32, status)
+        assert int(status) == 0
+        return o32
+
+    clean = prompt()
+    low = max(N_kv - N_q - window + 1, 0)
+    pad = -(-N_kv // 128) * 128
+    hidden = [j for j in range(pad) if sinks <= j < low or j >= N_kv]
+    sf = s1.k.sf.view(-1).view(2, 2, pad // 128, 1024)
+    at = [(j // 128, g // 4 * 512 + j % 32 * 16 + j % 128 // 32 * 4 + g % 4) for j in hidden for g in range(8)]
+    sf[:, :, [a for a, _ in at], [b for _, b in at]] = 0x7F
+    s1.delta.view(2, 4, pad)[:, :, hidden] = float("nan")
+    assert hidden and torch.equal(prompt(), clean) and bool(clean.any())
+
+
+# ------------------------------------------------------------------------------------------------------------------ many and long
+def test_weights_of_many_requests():
+    """More requests than the kernel holds lengths for, so that work items are found by another rule."""
+    lens = [0 if i % 97 == 3 else 1 + (37 * i) % 400 for i in range(780)] + [1500, 2047]
+    st = bounded.state(1600, lens, 4, 2)
+    old = random_sums(st, 4)
+    weights, _, o32, status = sums_of(st, st.page_table, old)
+    assert status == 0
+    for b, L in enumerate(lens):
+        assert torch.equal(weights[b, :, L:], old[b, :, L:])
+    for b in (0, 1, 3, 5, 100, 767, 768, 769, 779, 780, 781):
+        if lens[b]:
+            close_sums(weights[b, :, :lens[b]], old[b, :, :lens[b]], bounded.plain_weights(st, b), b)
+        else:
+            assert not o32[b].any()
+
+
+@pytest.mark.parametrize("nb,L,keep", [(1, 20000, 8000), (1, 70000, 9001), (40, 20000, 1000), (75, 49300, 200)])
+def test_the_tokens_of_long_rows_arrive(nb, L, keep):
+    """Rows of clusters, of one CTA and of more weights than are held: pools of random bytes, every kept token's bytes against those of the slot
+    that it comes from, pages that are not the call's left as they were.  Tables share the source pages (they are only read)."""
+    H_q, H_kv = 4, 2
+    per, pages = -(-keep // 64), -(-L // 64)
+    kv, table, spare = bounded.pool(1610 + nb, [L], H_q, H_kv, nb * per)
+    table, new_table = table.repeat(nb, 1), spare.view(nb, per)
+    lens = [L if b % 3 == 0 else (keep + 1, keep - 1)[b % 2] for b in range(nb)]
+    w = torch.rand(nb, H_kv, pages * 64, generator=torch.Generator().manual_seed(nb)).cuda()
+    before = bounded.copy_of(kv)
+    kept, new_lens, new_weights, status = bounded.evict(kv, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), w, keep, 4, 50, new_table)
+    assert status == 0 and new_lens.tolist() == [min(n, keep) for n in lens]
+    rest = torch.ones(kv.num_pages, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        rest[new_table[b, :-(-min(n, keep) // 64)].long()] = False
+    slot8, half = torch.arange(64, device="cuda") % 8, torch.arange(64, device="cuda") // 8
+
+    def tokens(x):
+        """[pages, H_kv, 64, 64 + 8 + 128 + 2 G] bytes of each token, by the maps of mpfa_paged_kv"""
+        k = x.k_codes.view(-1, H_kv, 64, 4, 16)
+        k = torch.take_along_dim(k, (torch.arange(4, device="cuda") ^ (slot8 // 2)[:, None]).view(1, 1, 64, 4, 1), 3).flatten(3)
+        v = x.v_fp8.view(-1, H_kv, 64, 8, 16)
+        v = torch.take_along_dim(v, (torch.arange(8, device="cuda") ^ slot8[:, None]).view(1, 1, 64, 8, 1), 3).flatten(3)
+        d = x.delta.view(torch.uint8).view(-1, H_kv, H_q // H_kv, 64, 2)
+        g = torch.arange(H_q // H_kv, device="cuda")
+        d = torch.stack([d[:, :, i][:, :, (half ^ i) * 8 + slot8] for i in g.tolist()], 3).flatten(3)
+        return torch.cat((k, x.k_sf.view(-1, H_kv, 64, 8), v, d), 3)
+
+    old, new = tokens(before), tokens(kv)
+    assert torch.equal(old[rest], new[rest])
+    for b, n in enumerate(lens):
+        m = min(n, keep)
+        for hk in range(H_kv):
+            at = kept[b, hk, :m].long()
+            assert bool((at[1:] > at[:-1]).all()) and int(at[0]) >= 0 and int(at[-1]) < n
+            rows = new[new_table[b].long(), hk].flatten(0, 1)
+            used = -(-m // 64) * 64
+            assert torch.equal(rows[:m], old[table[b, at // 64].long(), hk, at % 64]) and not rows[m:used].any()
+            assert torch.equal(new_weights[b, hk, :m], w[b, hk, at])
+    for b in (0, nb - 1):
+        assert np.array_equal(kept[b, 0, :min(lens[b], keep)].cpu().numpy(), plain.evicted(w[b, 0].cpu().numpy(), lens[b], keep, 4, 50))
+
+
+def test_a_budget_above_what_the_table_holds():
+    """Everything is kept, whatever the budget's share of sinks and newest tokens."""
+    kv, table, spare = bounded.pool(1620, [300, 5, 0], 8, 2, 3 * 16)
+    w, before = torch.rand(3, 2, table.shape[1] * 64, device="cuda"), bounded.copy_of(kv)
+    lens, new_table = torch.tensor([300, 5, 0], dtype=torch.int32, device="cuda"), spare.view(3, 16)
+    kept, new_lens, new_weights, status = bounded.evict(kv, table, lens, w, 1000, 600, 400, new_table)
+    assert status == 0
+    bounded.check_evicted(kv, before, table, [300, 5, 0], w, 1000, 600, 400, new_table, kept, new_lens, new_weights)
+
+
+def test_captured_steps_follow_the_lengths():
+    """A step with a window and one with weights, captured once and replayed on lengths from none to all that the table holds."""
+    B = binding()
+    st = bounded.state(1630, [3000, 3000, 3000], 8, 2)
+    table, old = st.page_table, random_sums(st, 7)
+    window_out, out, weights = torch.empty_like(st.out), torch.empty_like(st.out), old.clone()
+    window_ws = B.decode_window_workspace(3, 8, 2, table.shape[1], 1500, 70)
+    ws, status = B.decode_weights_workspace(3, 8, 2, table.shape[1]), torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def step():
+        B.mpfa_decode_window(st.q4, st.kv, table, st.seq_lens, st.stats, 1.0, 1500, 70, st.softmax_scale, window_out, None, window_ws, status)
+        B.mpfa_decode_weights(st.q4, st.kv, table, st.seq_lens, st.stats, 1.0, st.softmax_scale, weights, out, None, ws, status)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lens in ([0, 0, 0], [1, 3000, 0], [1024, 1025, 64], [2999, 2000, -4], [3000, 3000, 3000]):
+        st.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        weights.copy_(old)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        want, want_out, _, _ = sums_of(st, table, old)
+        assert torch.equal(weights, want) and torch.equal(out, want_out)
+        assert torch.equal(window_out, bounded.window_decode(st, 1500, 70)[0])
