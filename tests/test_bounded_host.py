@@ -77,6 +77,41 @@ def test_workspaces_follow_the_table_after_an_eviction(module, pages):
         assert st.workspace is was[0] and st.sums_workspace is was[1]
 
 
+@pytest.mark.parametrize("call", ["prefill_window", "prefill_paged_window", "decode_window", "decode_weights"])
+def test_tensors_that_the_library_would_misread_are_refused(monkeypatch, call):
+    """It is given addresses: strides, other types and other sizes go unseen there.  Refused before anything is called."""
+    from paper_2609_33135_b200 import binding as B
+    n = 1 if call.startswith("decode") else 9
+    good = dict(q=B.Fp4Tensor.empty(3, 8, n, "cpu"), kv=B.PagedKV.empty(4, 8, 2, device="cpu"), page_table=torch.zeros(3, 2, dtype=torch.int32),
+                seq_lens=torch.ones(3, dtype=torch.int32), stats=B.Stats.empty(3, 8, 2, "cpu"), v_scale=1.0, window=5, sinks=1, softmax_scale=0.1,
+                out=torch.empty(3, n, 8, 128, dtype=torch.bfloat16), out_f32=torch.empty(3, n, 8, 128), device_status=torch.zeros(1, dtype=torch.int32))
+    strided = torch.ones(3, 2, dtype=torch.int32)[:, 0]
+    bad = [{"out": torch.empty(3, n, 8, 128)}, {"out_f32": torch.empty(3, n, 8, 128, dtype=torch.bfloat16)}, {"out": good["out"][:2]},
+           {"out": torch.empty(3, n, 8, 256, dtype=torch.bfloat16)[..., :128]}, {"out_f32": torch.empty(3, n, 8, 256)[..., ::2]}]
+    if call == "prefill_window":
+        for name in ("kv", "page_table", "seq_lens"):
+            del good[name]
+        good.update(k=B.Fp4Tensor.empty(3, 2, 20, "cpu"), v_fp8=torch.zeros(3 * 2 * 128 * 128, dtype=torch.uint8), delta=None)
+    else:
+        bad += [{"seq_lens": strided}, {"seq_lens": good["seq_lens"].long()}, {"seq_lens": good["seq_lens"][:2]}, {"page_table": good["page_table"][:2]},
+                {"page_table": torch.zeros(2, 3, dtype=torch.int32).T}, {"page_table": good["page_table"].long()}]
+        if call == "prefill_paged_window":
+            bad += [{"q_lens": strided}, {"q_lens": good["seq_lens"][:2]}]
+        else:
+            good["workspace"] = torch.empty(1 << 16, dtype=torch.uint8)
+        if call == "decode_weights":
+            del good["window"], good["sinks"]
+            good["weights"] = torch.zeros(3, 2, 128)
+            bad += [{"weights": torch.zeros(3, 2, 256)[..., ::2]}, {"weights": torch.zeros(3, 2, 128, dtype=torch.float64)}, {"weights": torch.zeros(2, 2, 128)}]
+    made = []
+    monkeypatch.setattr(B, "_stream", lambda: made.append(1) or 0)
+    monkeypatch.setattr(B, "_check", lambda rc, name: None)
+    for change in bad:
+        with pytest.raises(AssertionError):
+            getattr(B, "mpfa_" + call)(**dict(good, **change))
+    assert not made
+
+
 def entries():
     """name -> kinds of all callables."""
     text = open(os.path.join(ROOT, "paper_2609_33135_b200", "csrc", "calls.c")).read()
