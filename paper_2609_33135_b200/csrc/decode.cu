@@ -60,15 +60,15 @@
 // exist (struct Span), by all roles alike, L too; only the look-up of a page uses the token's own index.  A page without a visible key is neither looked at nor
 // copied, so its table entry may be stale, and of the V rows of a page that is visible in part the others are zeros: a hidden token's V may
 // be anything, NaN included, and 0 x NaN is not 0.
-// Whole calls back to back: one request under a window of 1024 13.9 us (two kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
-// of cache) 87 us, 4.8 TB/s; 32 under 16384 (0.88 GB) 149 us, 5.9 TB/s.  Windows rarely end with a partition, so one item in five of the
-// 64 requests has one or two blocks, and such an item costs a microsecond more than its bytes do, by instruction fetch (2.0 stalled warps per
-// issue for want of an instruction, 0.6 where all items are long).  So what a role adds counts: masks made from tokens' own indices 91.4,
+// Whole calls back to back: one request under a window of 1024 13.7 us (two kernels' latency); 64 requests under 4095, 40:8 heads (0.42 GB
+// of cache) 87 us, 4.8 TB/s; 32 under 16384 (0.88 GB) 149 to 158 us on several boxes, 5.9 to 5.6 TB/s.  Windows rarely end with a partition, so
+// one item in five of the 64 requests has one or two blocks, and such an item costs a microsecond more than its bytes do, by instruction fetch
+// (1.1 to 1.2 stalled warps per issue for want of an instruction, 0.35 where all items are long).  So what a role adds counts: masks made from tokens' own indices 91.4,
 // with the window's bounds carried in every role's item 89.5; page ids of the item after a short one requested ahead 97.
 //
 // Weights.  The logits stay in FP32: 4 G bytes per key written, and read back by decode_weights_kernel once the merge has the (m, l) of the
-// whole request; recomputing them instead would read K, its scales and Delta_S again (72 + 2 G).  One request of 4097 keys 15.6 us (mpfa_decode
-// alone 12.9), 64 of 1000..8192, 40:8 heads, 118 (97.5; 0.55 GB of cache, and 0.1 of logits written and read).  Not kept: merge and sums in
+// whole request; recomputing them instead would read K, its scales and Delta_S again (72 + 2 G).  One request of 4097 keys 15.5 us (mpfa_decode
+// alone 12.9), 64 of 1000..8192, 40:8 heads, 118 to 121 (97.5; 0.55 GB of cache, and 0.1 of logits written and read).  Not kept: merge and sums in
 // one kernel (126 and 15.4); an L2 policy that lets the logits outlive the cache's bytes (they then come from L2, 12.5 us for the sums
 // instead of 15.5 alone, but the whole is no shorter: 119); the next chunk on its way during a sum, with 4 to 16 blocks per SM (118 to 119).
 #include <cuda_bf16.h>

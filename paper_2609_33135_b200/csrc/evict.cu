@@ -10,7 +10,7 @@
 // list's order decides nothing, so the order of the atomics does not show.  One read of the weights from memory: what comes after finds them
 // in shared memory, or in L2 where there are more than fit.
 // Bound by instructions and by barriers of 32 warps, not by memory: 8 heads of 4608 weights 8 us, 256 of 4200..9000 18 us (two CTAs to an
-// SM, 74 % of issue slots).  Not kept: three digits to the end and two scans of the block (25 us; 512 or 256 threads 16 us for the 8 heads),
+// SM, 74 to 77 % of issue slots).  Not kept: three digits to the end and two scans of the block (25 us; 512 or 256 threads 16 us for the 8 heads),
 // copies of the histogram by lane (no gain: 60 bins hold most counts, but the conflicts are not what it waits for).  One CTA to a row of 131072
 // weights: the whole call 164 us, by eight 30.5 (the rule and more figures stand at the launch; a row that is short in a wide table pays 3 us
 // for the cluster).
@@ -20,7 +20,7 @@
 // page is written once, in full, with the rest of it zeros.  Bound by memory: 32 requests x 8 heads x 4001 tokens, 0.21 GB read (0.26 from
 // DRAM: 2 bytes of Delta_S and 8 of scales out of 32-byte sectors) and as much written, 75 us alone, 5.8 TB/s; a thread to each piece with the
 // slots in shared memory, each kind of piece read and written in turn, 89.
-// Both, back to back: one request cut from 4608 to 4096 tokens 10.7 us, 32 cut from 4200..9000 to 4001 93.
+// Both, back to back: one request cut from 4608 to 4096 tokens 10.7 us (10.0 to 12.1), 32 cut from 4200..9000 to 4001 93 to 95.
 #include <cuda_bf16.h>
 
 #include "common.cuh"

@@ -221,7 +221,7 @@ __device__ __forceinline__ float exponent_unit(const PrefillParams &p, int b) {
 // row; everything else is a matter of addresses and masks (struct Tile, visible32()).  An item has up to five blocks with a mask (the window's
 // two ends lie in two blocks each, the sinks' last block) where the causal kernel has one or two, so masks are made as sets of 32 bits and
 // voted on per 32 keys: compared key by key, 4001 tokens under 1024 (32:8 heads) took 77 us, 16384 under 4096 821, chunks of 512 under 2048 on
-// pages 164; so 73, 766 and 98 (0.80, 1.27 and 0.70 PFLOP/s of visible pairs; a window as wide as the context costs what causal attention
+// pages 164; so 73, 766 to 783 on several boxes, and 97 to 98 (0.81, 1.27 to 1.25 and 0.71 PFLOP/s of visible pairs; a window as wide as the context costs what causal attention
 // costs, on pages 5 % more).  Contiguous operands take the first form of LONG at every length (16384 under 4096 766 / 806, 4001 under 1024 73 /
 // 78), pages the second (2048-key windows 111 / 96; windows of 512 keys 51 / 53).
 // What bounds it is what bounds the causal kernel, a chain of hand-overs per block and the accumulator's per item; of what is visited, one
