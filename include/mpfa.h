@@ -384,6 +384,7 @@ mpfa_status mpfa_decode_weights(const mpfa_fp4_tensor *h_q, const mpfa_paged_kv 
  *   new_weights [B, H_kv, new_weights_stride]  the kept tokens' weights, zeros after them (where new tokens' sums start).
  * weights_stride >= 64 * max_pages_per_req, new_weights_stride >= keep, sinks + recent <= keep, and new_weights and new_lens overlap weights
  * and seq_lens nowhere (else MPFA_ERR_INVALID_ARG).  seq_lens[b] above 64 * max_pages_per_req is treated as that bound.
+ * Which tokens are kept is undefined where the weights change while the call reads them (a step of another stream that adds to them).
  * A page-table entry outside [0, num_pages) raises MPFA_DEV_BAD_PAGE: tokens of such a source page become zeros, a page of new_table is left
  * out.  Decode works on the new pages as on any; since the kv heads keep different tokens, a slot no longer is a position. */
 mpfa_status mpfa_evict_paged(const mpfa_paged_kv *h_kv, const int32_t *page_table, int B, int max_pages_per_req,

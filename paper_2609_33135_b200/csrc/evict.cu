@@ -98,7 +98,8 @@ struct Team {
 
 // This CTA's part [begin, end) of a row of n > keep slots: those that stay, to kept[] in ascending order.  HELD: `held` has the orders of the
 // part's weights (from held[0] on), and sh.hist the counts of its candidates' first digits; otherwise both are made from the weights w in
-// global memory.
+// global memory.  Those are read in each pass, and a program that goes on adding to them meanwhile makes the passes disagree: then a bin may not
+// be found, more be listed than were counted, and more stay than the row has room for, so each of the three has its own bound there.
 template <bool CLUSTER, bool HELD>
 __device__ __forceinline__ void select_tokens(const EvictParams &p, const Team<CLUSTER> &team, const uint32_t *held, const float *w, int n, int begin,
                                               int end, int32_t *kept, SelectShared &sh) {
@@ -115,7 +116,10 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const Team<C
     bool by_slot = false, counted = HELD;
 #pragma unroll 1
     for (uint32_t inside = (uint32_t)(n - p.recent - p.sinks); inside > LIST; counted = false) {
-      if (shift == 0) shift = 32, by_slot = true;
+      if (shift == 0) {
+        if (!HELD && by_slot) break;
+        shift = 32, by_slot = true;
+      }
       const int bits = min(DIGIT, shift);
       shift -= bits;
       const uint32_t digit = (1u << bits) - 1u;
@@ -190,16 +194,17 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const Team<C
         const uint64_t key = (uint64_t)u << 32 | s;
         if (CLUSTER) {
           const uint32_t at = cluster_add(cluster_address(smem_u32(&sh.listed), 0), 1u);
-          cluster_store(cluster_address(smem_u32(&sh.list[0]), 0) + 8 * at, key);
+          if (HELD || at < LIST) cluster_store(cluster_address(smem_u32(&sh.list[0]), 0) + 8 * at, key);
         } else {
-          sh.list[atomicAdd(&sh.listed, 1u)] = key;
+          const uint32_t at = atomicAdd(&sh.listed, 1u);
+          if (HELD || at < LIST) sh.list[at] = key;
         }
       }
     }
     team.sync();
     // four threads to a candidate
     if (!CLUSTER || team.r == 0) {
-      const int m = (int)sh.listed;
+      const int m = HELD ? (int)sh.listed : min((int)sh.listed, LIST);
       if (warp * 8 < m) {
         const uint64_t mine = (t >> 2) < m ? sh.list[t >> 2] : ~0ull;
         uint32_t larger = 0;
@@ -242,7 +247,8 @@ __device__ __forceinline__ void select_tokens(const EvictParams &p, const Team<C
 #pragma unroll 2
   for (int i0 = from, k = 0; i0 < until; i0 += 32, ++k) {
     const uint32_t bits = k < 32 ? __shfl_sync(0xffffffffu, answers, k) : __ballot_sync(0xffffffffu, stays(i0 + lane));
-    if (bits >> lane & 1u) kept[to + __popc(bits & ((1u << lane) - 1u))] = i0 + lane;
+    const uint32_t at = to + __popc(bits & ((1u << lane) - 1u));
+    if ((bits >> lane & 1u) && (HELD || at < (uint32_t)p.keep)) kept[at] = i0 + lane;
     to += __popc(bits);
   }
 }
@@ -314,9 +320,10 @@ __global__ void __launch_bounds__(MOVE_THREADS, 8) evict_move_kernel(const __gri
   grid_dependency_wait();
   const int at = page * PAGE + warp * 8 + (lane & 7);   // lane l: token l mod 8
   const int to = p.new_table[(size_t)b * p.new_pages + page];
-  const int from = at < p.keep ? p.kept[((size_t)b * p.H_kv + hk) * p.keep + at] : -1;   // -1 past the last token
-  const int count = min(p.length(b), p.keep);
+  int from = at < p.keep ? p.kept[((size_t)b * p.H_kv + hk) * p.keep + at] : -1;   // -1 past the last token
+  const int n = p.length(b), count = min(n, p.keep);
   if (page * PAGE >= count) return;
+  if (from >= n) from = -1;   // not written by a selection whose weights changed (select_tokens): what was there before
   if (from >= 0 && lane < 8) {
     const size_t head = (size_t)b * p.H_kv + hk;
     p.new_weights[head * p.new_stride + at] = p.weights[head * p.weights_stride + from];

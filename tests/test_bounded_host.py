@@ -140,3 +140,16 @@ def test_conversions_and_what_is_refused(name):
         for x in {"i": (1 << 31, -(1 << 31) - 1, 1 << 70), "z": (-1, 1 << 64)}.get(c, ()):
             with pytest.raises(OverflowError):
                 call(*null[:k], x, *null[k + 1:])
+
+
+def test_eviction_bounds_what_changing_weights_could_break():
+    """Where a row's weights do not fit shared memory each pass reads them again.  Weights that change between the passes must not make the
+    search for the border endless, the list longer than its memory, a row longer than its budget, or a token's slot one that does not exist."""
+    from test_launch_rule import bodies, code
+    select, move = bodies(code("evict.cu"))["select_tokens"][1], bodies(code("evict.cu"))["evict_move_kernel"][1]
+    assert re.search(r"if \(!HELD && by_slot\) break;", select)
+    for write in re.findall(r"[^;{}]*(?:sh\.list\[at\] = key|8 \* at, key\)|kept\[at\] = )", select):
+        assert re.search(r"HELD \|\| at < (LIST|\(uint32_t\)p\.keep)", write), write
+    assert len(re.findall(r"sh\.list\[\w+\] = |, key\);|kept\[[^\]]*\] = ", select)) == 3
+    assert re.search(r"min\(\(int\)sh\.listed, LIST\)", select)
+    assert 0 < move.index("if (from >= n) from = -1") < move.index("p.weights[head * p.weights_stride + from]")

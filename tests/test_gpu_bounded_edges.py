@@ -443,3 +443,35 @@ def test_captured_steps_follow_the_lengths():
         want, want_out, _, _ = sums_of(st, table, old)
         assert torch.equal(weights, want) and torch.equal(out, want_out)
         assert torch.equal(window_out, bounded.window_decode(st, 1500, 70)[0])
+
+
+@pytest.mark.parametrize("nb,L,keep", [(75, 49300, 4000), (1, 400000, 60000)])   # one CTA to a row; clusters
+def test_weights_that_change_during_an_eviction_do_no_harm(nb, L, keep):
+    """Which tokens are kept is undefined then; the call ends, and writes nothing beside its buffers."""
+    B = binding()
+    per, pages = -(-keep // 64), -(-L // 64)
+    kv = B.PagedKV.empty(pages + nb * per, 1, 1)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(nb, 1)
+    new_table = torch.arange(pages, pages + nb * per, dtype=torch.int32, device="cuda").view(nb, per)
+    lens = torch.full((nb,), L, dtype=torch.int32, device="cuda")
+    w = torch.rand(nb, 1, pages * 64, device="cuda")
+    guard, n = 4096, nb * keep
+    arena = torch.full((2 * n + 3 * guard,), -(2 ** 30), dtype=torch.int32, device="cuda")
+    kept, new_weights = arena[guard:guard + n].view(nb, 1, keep), arena[2 * guard + n:2 * guard + 2 * n].view(torch.float32).view(nb, 1, keep)
+    new_lens, status = torch.empty_like(lens), torch.zeros(1, dtype=torch.int32, device="cuda")
+    values = [torch.rand_like(w), torch.rand_like(w) * 1e-6, torch.full_like(w, 0.5)]
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(100):
+        B.mpfa_evict_paged(kv, table, lens, w, keep, 4, 100, new_table, kept, new_lens, new_weights, status)
+        with torch.cuda.stream(other):
+            for v in values:
+                w.copy_(v)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and new_lens.tolist() == [keep] * nb
+    for a, b in ((0, guard), (guard + n, 2 * guard + n), (2 * guard + 2 * n, arena.numel())):
+        assert bool((arena[a:b] == -(2 ** 30)).all())
+    w.copy_(values[0])   # and with weights that stay, what is always kept
+    B.mpfa_evict_paged(kv, table, lens, w, keep, 4, 100, new_table, kept, new_lens, new_weights, status)
+    for b in (0, nb - 1):
+        assert np.array_equal(kept[b, 0].cpu().numpy(), plain.evicted(w[b, 0].cpu().numpy(), L, keep, 4, 100))
