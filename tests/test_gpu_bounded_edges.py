@@ -475,3 +475,28 @@ def test_weights_that_change_during_an_eviction_do_no_harm(nb, L, keep):
     B.mpfa_evict_paged(kv, table, lens, w, keep, 4, 100, new_table, kept, new_lens, new_weights, status)
     for b in (0, nb - 1):
         assert np.array_equal(kept[b, 0].cpu().numpy(), plain.evicted(w[b, 0].cpu().numpy(), L, keep, 4, 100))
+
+
+@pytest.mark.parametrize("window,sinks", [(30, 2), (1000, 0), (1, 200)])
+def test_a_chunk_longer_than_its_context(window, sinks):
+    """Its first queries stand before the first key and see nothing, a whole tile of them among others; one request has no key at all."""
+    B = binding()
+    lens, N_q, H_q, H_kv = [150, 290, 1, 0], 300, 4, 2
+    st = bounded.state(1640, lens, H_q, H_kv)
+    q4 = B.Fp4Tensor.empty(4, H_q, N_q)
+    B.mpfa_quantize_qk(torch.randn(4, N_q, H_q, 128, generator=torch.Generator().manual_seed(8)).bfloat16().cuda(), None,
+                       B.MPFA_SMOOTH | B.MPFA_STATS_FROZEN, st.stats, q4, None, None, None)
+    out = torch.full((4, N_q, H_q, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    o32, status = torch.full((4, N_q, H_q, 128), 7.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mpfa_prefill_paged_window(q4, st.kv, st.page_table, st.seq_lens, st.stats, 1.0, window, sinks, st.softmax_scale, out, o32, status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    bounded.rounded(out, o32)
+    Q = plain.tile_rows(q4)
+    for b, L in enumerate(lens):
+        got = o32[b].cpu().numpy()
+        assert not got[:N_q - L].any()
+        if L:
+            K, V, D = plain.cached(st.kv, st.page_table[b].cpu().numpy(), L)
+            bounded.check_rows(Q[b], K, V, D, got, np.arange(N_q) + L - N_q, window, sinks, plain.lam_of(st.stats, b, st.softmax_scale), 1.0,
+                               (H_q, H_kv), b)
