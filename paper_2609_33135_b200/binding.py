@@ -421,14 +421,14 @@ def decode_weights_workspace(B: int, H_q: int, H_kv: int, max_pages: int, device
 
 
 def _outputs(q: Fp4Tensor, out: torch.Tensor, out_f32: Optional[torch.Tensor]) -> bool:
-    """Whether the outputs are what the library writes for these queries: it is given their addresses only."""
+    """Whether the outputs have room for what the library writes for these queries: it is given their addresses only."""
     n = q.B * q.H * q.N * HEAD_DIM
-    return (out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == n
-            and (out_f32 is None or (out_f32.dtype == torch.float32 and out_f32.is_contiguous() and out_f32.numel() == n)))
+    return (out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n
+            and (out_f32 is None or (out_f32.dtype == torch.float32 and out_f32.is_contiguous() and out_f32.numel() >= n)))
 
 
 def _per_request(n: int, lens: torch.Tensor) -> bool:
-    return lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == n
+    return lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() >= n
 
 
 def mpfa_prefill_window(q: Fp4Tensor, k: Fp4Tensor, v_fp8: torch.Tensor, delta: Optional[torch.Tensor], stats: Stats, v_scale: float,
@@ -445,7 +445,7 @@ def mpfa_prefill_paged_window(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tenso
                               window: int, sinks: int, softmax_scale: float, out: torch.Tensor, out_f32: Optional[torch.Tensor],
                               device_status: torch.Tensor, q_lens: Optional[torch.Tensor] = None) -> None:
     """mpfa_prefill_paged where each query sees the last `window` keys and the first `sinks`."""
-    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] == q.B
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] >= q.B
     assert _per_request(q.B, seq_lens) and (q_lens is None or _per_request(q.B, q_lens)) and _outputs(q, out, out_f32)
     rc = lib().packed_mpfa_prefill_paged_window(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),
                                                 _ptr(q_lens), stats.packed_stats(), v_scale, window, sinks, softmax_scale, _ptr(out),
@@ -457,7 +457,7 @@ def mpfa_decode_window(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq_
                        window: int, sinks: int, softmax_scale: float, out: torch.Tensor, out_f32: Optional[torch.Tensor],
                        workspace: torch.Tensor, device_status: torch.Tensor) -> None:
     """mpfa_decode where the query sees the last `window` keys and the first `sinks`; workspace: decode_window_workspace()."""
-    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] == q.B
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] >= q.B
     assert _per_request(q.B, seq_lens) and _outputs(q, out, out_f32)
     rc = lib().packed_mpfa_decode_window(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),
                                          stats.packed_stats(), v_scale, window, sinks, softmax_scale, _ptr(out), _ptr(out_f32),
@@ -470,7 +470,7 @@ def mpfa_decode_weights(q: Fp4Tensor, kv: PagedKV, page_table: torch.Tensor, seq
                         workspace: torch.Tensor, device_status: torch.Tensor) -> None:
     """mpfa_decode that adds each key's softmax weights to weights [B, H_kv, >= 64 * pages] (float32); workspace:
     decode_weights_workspace()."""
-    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] == q.B
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] >= q.B
     assert _per_request(q.B, seq_lens) and _outputs(q, out, out_f32)
     assert weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape[:2] == (q.B, kv.H_kv)
     rc = lib().packed_mpfa_decode_weights(q.packed_fp4(), kv.packed_paged(), _ptr(page_table), page_table.shape[1], _ptr(seq_lens),

@@ -110,6 +110,11 @@ def test_tensors_that_the_library_would_misread_are_refused(monkeypatch, call):
         with pytest.raises(AssertionError):
             getattr(B, "mpfa_" + call)(**dict(good, **change))
     assert not made
+    larger = {"out": torch.empty(5, n, 8, 128, dtype=torch.bfloat16), "out_f32": None, "seq_lens": torch.ones(7, dtype=torch.int32),
+              "page_table": torch.zeros(7, 2, dtype=torch.int32)}   # buffers of a larger batch
+    monkeypatch.setattr(B, "lib", lambda: type("Lib", (), {"packed_mpfa_" + call: staticmethod(lambda *a: 0)}))
+    getattr(B, "mpfa_" + call)(**dict(good, **{k: v for k, v in larger.items() if k in good}))
+    assert made
 
 
 def entries():
