@@ -20,7 +20,7 @@
 // page is written once, in full, with the rest of it zeros.  Bound by memory: 32 requests x 8 heads x 4001 tokens, 0.21 GB read (0.26 from
 // DRAM: 2 bytes of Delta_S and 8 of scales out of 32-byte sectors) and as much written, 75 us alone, 5.8 TB/s; a thread to each piece with the
 // slots in shared memory, each kind of piece read and written in turn, 89.
-// Both, back to back: one request cut from 4608 to 4096 tokens 10.7 us (10.0 to 12.1), 32 cut from 4200..9000 to 4001 93 to 95.
+// Both, back to back: one request cut from 4608 to 4096 tokens 10.7 us (9.8 to 12.1), 32 cut from 4200..9000 to 4001 93 to 95.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
